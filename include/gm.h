@@ -409,6 +409,121 @@ int gm_check_error(gm_model *m, int32_t *code, int32_t *index);
  * Synchronises the device. */
 int gm_flush_effects(gm_model *m, gm_effect_cb cb, void *user, int32_t *n_dropped);
 
+/* ------------------------------------------------------------ operators
+ * Attention and KV-cache operators on caller tensors, without a model: a
+ * cache held in 8 or 4 bits (gm_kv_write, gm_kv_read), attention of new
+ * tokens over it (gm_attention_cached), and attention over whole prompts with
+ * modified scores (gm_attention).  A model created with gm_model_create_ex
+ * runs the same kernels.  They only enqueue on `stream`: no host
+ * synchronisation, no allocation, capturable.  All pointers are device
+ * pointers of the current device; a bad argument that the host can see gives
+ * GM_E_INVAL and nothing is enqueued.  Calls that share no output and no
+ * workspace may overlap. */
+
+/* A tensor [batch, tokens, heads, head_dim] whose channels are contiguous:
+ * element (b, t, h, c) is at p[b * batch + t * token + h * head + c], strides
+ * in elements.  p and the strides of dimensions longer than one must be
+ * multiples of 16 bytes; strides may not be negative.  An output's elements may
+ * not overlap one another or an input. */
+typedef struct gm_tensor {
+  void* p;
+  int64_t batch, token, head;
+} gm_tensor;
+
+/* A KV cache of one layer in 8 or 4 bits.  head_dim is 32, 64 or 128; max_seq
+ * a multiple of 64.  A group is 32 consecutive channels of one position and
+ * head, with Q = 127 (8 bits) or 7 (4 bits) and a = max |x| over the group:
+ *   scale = bf16(a * fl32(1 / Q))            (the product in fp32)
+ *   code  = x / scale rounded to the nearest integer, ties to even, limited to
+ *           [-Q, Q]; 0 where scale is 0
+ *   value = code * scale
+ * A group holding an Inf or NaN is stored as NaN (scale NaN), all of it.
+ *  k, v  codes plus 2^(bits - 1), unsigned, 16-byte aligned:
+ *        [batch][heads][max_seq][head_dim] bytes, or for 4 bits
+ *        [batch][heads][max_seq][head_dim / 2] bytes, channel 2i in the low half
+ *  k_scale, v_scale  bfloat16 [batch][heads][head_dim / 32][max_seq], 16-byte
+ *        aligned
+ *  valid bytes [batch][max_seq], 8-byte aligned: 0 hides the position from
+ *        attention; or NULL: every position may be attended */
+typedef struct gm_kv_cache {
+  int32_t bits, batch, heads, max_seq, head_dim;
+  void *k, *v, *k_scale, *v_scale;
+  uint8_t* valid;
+} gm_kv_cache;
+
+/* Store k and v rows [B, n, heads, head_dim] of `dtype` (B <= cache->batch):
+ * row i of sequence b goes to position start[b] + i, for i < count[b] (NULL:
+ * all n rows; start NULL: 0).  Positions outside [0, max_seq) are not stored;
+ * everything else in the cache keeps its value.  With cache->valid the
+ * position's byte becomes mask[b * n + i] != 0 (mask NULL: 1).  start, count:
+ * int32 [B]; mask: int32 [B, n]. */
+int gm_kv_write(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n, gm_tensor k,
+                gm_tensor v, const int32_t* start, const int32_t* count, const int32_t* mask,
+                hipStream_t stream);
+
+/* Read rows back into k and v [B, n, heads, head_dim] of `dtype` (each value
+ * rounded once): row i of sequence b from position start[b] + i.  Rows at or
+ * past count[b], and positions outside [0, max_seq), read as zeros. */
+int gm_kv_read(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n,
+               const int32_t* start, const int32_t* count, gm_tensor k, gm_tensor v,
+               hipStream_t stream);
+
+/* How a score is made from q.k.  scale multiplies it; then, with softcap > 0,
+ * s = softcap * tanh(s / softcap); then, with slopes (fp32 [n_heads] of the
+ * query heads, or NULL), s -= slopes[h] * |query position - key position|. */
+typedef struct gm_scores {
+  float scale, softcap;
+  const float* slopes;
+} gm_scores;
+
+/* Attention of the Sq newest tokens of each sequence over the cache, which
+ * already holds them: query i of sequence b is at position lengths[b] - Sq + i
+ * and sees the valid positions up to its own; a query that sees none gives
+ * zeros.  lengths: int32 [B], read on the device, at most max_seq (larger ones
+ * count as max_seq).  q and out: [B, Sq, n_heads, head_dim] of `dtype`,
+ * n_heads a multiple of cache->heads; query head h reads key head
+ * h / (n_heads / cache->heads).  Softmax statistics and sums are fp32; for
+ * 16-bit dtypes a probability times a value's scale is rounded to 16 bits of
+ * 11 significant bits.
+ * workspace: device, 16-byte aligned, at least
+ * gm_attention_cached_workspace(...) bytes (which may be 0: then NULL will do),
+ * used by this call alone until it has run. */
+typedef struct gm_cached_attention {
+  const gm_kv_cache* cache;
+  int32_t dtype, B, Sq, n_heads;
+  gm_tensor q, out;
+  const int32_t* lengths;
+  gm_scores scores;
+  void* workspace;
+  uint64_t workspace_bytes;
+} gm_cached_attention;
+int gm_attention_cached(const gm_cached_attention* a, hipStream_t stream);
+uint64_t gm_attention_cached_workspace(const gm_kv_cache* cache, int32_t dtype, int32_t B,
+                                       int32_t Sq, int32_t n_heads);
+
+/* Attention over whole prompts.  Query i of a sequence is at position
+ * i + q_offset, key j at position j.  Query i sees key j when all of these
+ * hold:
+ *   key_mask is NULL or key_mask[b, j] != 0            (int32 [B, Sk])
+ *   q_doc is NULL or q_doc[b, i] == k_doc[b, j]        (int32 [B, Sq], [B, Sk])
+ *   causal is 0, or j <= i + q_offset, or j < prefix[b]
+ *                                        (prefix: int32 [B], or NULL for none)
+ * A query that sees no key gives zeros; what a hidden key or value holds, Inf
+ * and NaN among it, does not reach a query it is hidden from.
+ * head_dim is 32, 64 or 128; n_heads a multiple of kv_heads, query head h
+ * reading key head h / (n_heads / kv_heads).  q and out are
+ * [B, Sq, n_heads, head_dim], k and v [B, Sk, kv_heads, head_dim], all of
+ * `dtype`.  |q_offset| + Sq and Sk must be below 2^24.  Softmax statistics and
+ * sums are fp32; 16-bit probabilities are rounded to `dtype`. */
+typedef struct gm_prompt_attention {
+  int32_t dtype, B, Sq, Sk, n_heads, kv_heads, head_dim;
+  gm_tensor q, k, v, out;
+  int32_t causal, q_offset;
+  gm_scores scores;
+  const int32_t *key_mask, *q_doc, *k_doc, *prefix;
+} gm_prompt_attention;
+int gm_attention(const gm_prompt_attention* a, hipStream_t stream);
+
 /* No passage: test instrumentation for per-layer parity.
  * The forward of gm_forward_ex (pre-norm models), enqueued on `stream`
  * without a graph and as one branch, copying every layer's storage points

@@ -13,17 +13,13 @@
 
 #include "gm.h"
 #include "gm_device.h"
+#include "gm_error.h"
 #include "gm_kernels.h"
 
 namespace gm {
 void attention_set_order(int o);
-}
 
-using namespace gm;
-
-namespace {
-
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 int hip_fail(hipError_t e, const char* what) {
   g_last_error = std::string(what) + ": " + hipGetErrorString(e);
@@ -33,12 +29,11 @@ int inval(const char* what) {
   g_last_error = what;
   return GM_E_INVAL;
 }
+}  // namespace gm
 
-#define HIP_TRY(call)                                   \
-  do {                                                  \
-    hipError_t e_ = (call);                             \
-    if (e_ != hipSuccess) return hip_fail(e_, #call);   \
-  } while (0)
+using namespace gm;
+
+namespace {
 
 struct LayerBufs {
   void *ln1_g = nullptr, *ln1_b = nullptr, *wqkv = nullptr, *bqkv = nullptr;

@@ -28,6 +28,7 @@ GM_EFFECT_PAD, GM_EFFECT_REGROW, GM_EFFECT_CLAMP, GM_EFFECT_LOG = 1, 2, 3, 4
 GM_ROPE_PLAIN, GM_ROPE_LONG_SHORT = 0, 1
 
 _i32, _f32, _u64, _vp = ctypes.c_int32, ctypes.c_float, ctypes.c_uint64, ctypes.c_void_p
+_i64 = ctypes.c_int64
 
 
 class gm_config(ctypes.Structure):
@@ -94,6 +95,34 @@ class gm_kernel_time(ctypes.Structure):
                 ("bytes", ctypes.c_double)]
 
 
+class gm_tensor(ctypes.Structure):
+    _fields_ = [("p", _vp), ("batch", _i64), ("token", _i64), ("head", _i64)]
+
+
+class gm_kv_cache(ctypes.Structure):
+    _fields_ = [("bits", _i32), ("batch", _i32), ("heads", _i32), ("max_seq", _i32),
+                ("head_dim", _i32), ("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp),
+                ("valid", _vp)]
+
+
+class gm_scores(ctypes.Structure):
+    _fields_ = [("scale", _f32), ("softcap", _f32), ("slopes", _vp)]
+
+
+class gm_cached_attention(ctypes.Structure):
+    _fields_ = [("cache", ctypes.POINTER(gm_kv_cache)), ("dtype", _i32), ("B", _i32), ("Sq", _i32),
+                ("n_heads", _i32), ("q", gm_tensor), ("out", gm_tensor), ("lengths", _vp),
+                ("scores", gm_scores), ("workspace", _vp), ("workspace_bytes", _u64)]
+
+
+class gm_prompt_attention(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("B", _i32), ("Sq", _i32), ("Sk", _i32), ("n_heads", _i32),
+                ("kv_heads", _i32), ("head_dim", _i32), ("q", gm_tensor), ("k", gm_tensor),
+                ("v", gm_tensor), ("out", gm_tensor), ("causal", _i32), ("q_offset", _i32),
+                ("scores", gm_scores), ("key_mask", _vp), ("q_doc", _vp), ("k_doc", _vp),
+                ("prefix", _vp)]
+
+
 KERNEL_KINDS = ["prologue", "rope_fill", "embed", "norm", "gemm_qkv", "attention",
                 "gemm_o", "gemm_up", "gemm_down", "gemm_head", "effects", "kv_store",
                 "argmax", "log", "gemm_xq", "gemm_xkv", "gemm_xo", "xattn"]
@@ -105,6 +134,8 @@ EXPORTS = ["gm_model_create", "gm_model_destroy", "gm_forward", "gm_forward_ex",
            "gm_profile_forward", "gm_set_exec_mode", "gm_set_graph_mode", "gm_read_decisions", "gm_decisions_device_ptr",
            "gm_check_error", "gm_flush_effects", "gm_debug_buffer", "gm_debug_forward_layers",
            "gm_get_stats", "gm_forward_noalloc",
+           "gm_kv_write", "gm_kv_read", "gm_attention_cached", "gm_attention_cached_workspace",
+           "gm_attention",
            "gm_strerror",
            "gm_last_error"]
 
@@ -143,14 +174,22 @@ def lib(path: str = LIB_PATH) -> ctypes.CDLL:
     L.gm_debug_buffer.argtypes = [_vp, _i32, ctypes.POINTER(_vp), ctypes.POINTER(_u64)]
     L.gm_debug_forward_layers.argtypes = [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _u64]
     L.gm_get_stats.argtypes = [_vp, ctypes.POINTER(gm_stats)]
+    L.gm_kv_write.argtypes = [ctypes.POINTER(gm_kv_cache), _i32, _i32, _i32, gm_tensor, gm_tensor,
+                              _vp, _vp, _vp, _vp]
+    L.gm_kv_read.argtypes = [ctypes.POINTER(gm_kv_cache), _i32, _i32, _i32, _vp, _vp, gm_tensor,
+                             gm_tensor, _vp]
+    L.gm_attention_cached.argtypes = [ctypes.POINTER(gm_cached_attention), _vp]
+    L.gm_attention_cached_workspace.argtypes = [ctypes.POINTER(gm_kv_cache), _i32, _i32, _i32, _i32]
+    L.gm_attention.argtypes = [ctypes.POINTER(gm_prompt_attention), _vp]
     L.gm_strerror.argtypes = [ctypes.c_int]
     L.gm_strerror.restype = ctypes.c_char_p
     L.gm_last_error.argtypes = []
     L.gm_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("gm_model_destroy", "gm_decisions_device_ptr", "gm_strerror",
-                        "gm_last_error"):
+                        "gm_last_error", "gm_attention_cached_workspace"):
             getattr(L, name).restype = ctypes.c_int
+    L.gm_attention_cached_workspace.restype = _u64
     _lib = L
     return L
 
@@ -307,3 +346,29 @@ def gm_get_stats(m: int) -> gm_stats:
 
 def gm_strerror(code: int) -> str:
     return lib().gm_strerror(code).decode()
+
+
+def gm_kv_write(cache: gm_kv_cache, dtype: int, B: int, n: int, k: gm_tensor, v: gm_tensor,
+                start: Optional[int], count: Optional[int], mask: Optional[int],
+                stream: int) -> None:
+    _check(lib().gm_kv_write(ctypes.byref(cache), dtype, B, n, k, v, start, count, mask, stream),
+           "gm_kv_write")
+
+
+def gm_kv_read(cache: gm_kv_cache, dtype: int, B: int, n: int, start: Optional[int],
+               count: Optional[int], k: gm_tensor, v: gm_tensor, stream: int) -> None:
+    _check(lib().gm_kv_read(ctypes.byref(cache), dtype, B, n, start, count, k, v, stream),
+           "gm_kv_read")
+
+
+def gm_attention_cached(a: gm_cached_attention, stream: int) -> None:
+    _check(lib().gm_attention_cached(ctypes.byref(a), stream), "gm_attention_cached")
+
+
+def gm_attention_cached_workspace(cache: gm_kv_cache, dtype: int, B: int, Sq: int,
+                                  n_heads: int) -> int:
+    return lib().gm_attention_cached_workspace(ctypes.byref(cache), dtype, B, Sq, n_heads)
+
+
+def gm_attention(a: gm_prompt_attention, stream: int) -> None:
+    _check(lib().gm_attention(ctypes.byref(a), stream), "gm_attention")
