@@ -3,7 +3,10 @@
 // prefix masks next to the causal one; query heads may share key heads.
 #include <math.h>
 
+#include <type_traits>
+
 #include "gm_device.h"
+#include "gm_flash.h"
 #include "gm_ops.h"
 
 namespace gm {
@@ -89,12 +92,420 @@ void prompt_rows(const gm_prompt_attention& a, hipStream_t s) {
   else hipLaunchKernelGGL((k_prompt_rows<T, 128>), grid, block, 0, s, a);
 }
 
+// ------------------------------------------------------------ 16-bit, head size 64 and 128
+// 32 bits of four consecutive int32, at any 4-byte address.
+typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+
+constexpr int kTileWords = 128;   // key tiles a workgroup keeps a bit for: 32 a word (262144 keys)
+
+// Workgroup = 128 queries of one (sequence, head), as k_flash (gm_attention.hip)
+// splits and multiplies: 4 wavefronts x 32 queries, key and value tiles of 64 keys
+// double-buffered in LDS, S^T = K Q^T and O^T += V^T P^T on 32x32x16, a lane
+// holding 32 scores of one query per tile, the running maximum moved lazily.
+// What the scores go through instead:
+//  CAP   softcap tanh(x / softcap) = C - 2 C / (exp2(x c2) + 1) in log2 units, C =
+//        softcap log2(e): two transcendental and three other instructions
+//  BIAS  one subtraction and one fma with the distance
+//  masks a 64-bit word per lane and tile: key mask (a ballot of wavefront 0), causal
+//        and prefix bounds (shifts) and documents (32 comparisons where the tile or
+//        the wavefront's queries hold more than one); none at all for a tile that is
+//        open to every query of the wavefront.
+// Tiles without a visible key for the workgroup are not fetched: with a key mask or
+// documents every workgroup first marks the tiles that hold an unmasked key whose
+// document lies in the range of its queries' (any order of documents is right;
+// packed ones in order skip nearly all others).
+// A hidden key has probability 0, but 0 times an Inf or NaN value is NaN in the
+// matrix product.  Such a product is never finite, so queries whose sums came out
+// not finite are computed again by prompt_row, which skips hidden keys; the loop
+// itself checks nothing.
+template <typename T, int HD, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void k_prompt_flash(gm_prompt_attention a) {
+  constexpr int QB = 128, KB = 64, NW = 4;
+  typedef typename Mfma32A<T>::vec vec;
+  constexpr int KS = HD / 16;                 // k steps of S^T (head dim)
+  constexpr int CB = HD / 32;                 // 32-channel blocks of O^T
+  constexpr int CPR = HD / 8;                 // 16-byte chunks per key row
+  constexpr int RPL = 16 / CPR;               // key rows per 256 bytes
+  constexpr int RPI = 64 / CPR;               // key rows per 1 KB copy instruction
+  constexpr int LPW = KB / RPI / NW;          // copy instructions per wavefront, tile and operand
+  constexpr int TILE = KB * HD;
+  __shared__ __attribute__((aligned(1024))) T sK0[TILE];
+  __shared__ __attribute__((aligned(1024))) T sK1[TILE];
+  __shared__ __attribute__((aligned(1024))) T sV0[TILE];
+  __shared__ __attribute__((aligned(1024))) T sV1[TILE];
+  __shared__ __attribute__((aligned(16))) int sDoc[2][KB];
+  __shared__ unsigned long long sBits[2];     // key not masked (bit per key)
+  __shared__ int sOne[2];                     // the tile's keys are of one document
+  __shared__ uint32_t sTiles[kTileWords];
+
+  // query blocks outermost, heaviest first; the heads of a group next to one
+  // another in steps of 8 workgroups where the key heads allow (one XCD, one L2)
+  const int nqb = (a.Sq + QB - 1) / QB, P = a.B * a.n_heads;
+  int p = blockIdx.x;
+  {
+    constexpr int kSlot = 256;
+    const int sl = p / kSlot;
+    if ((sl & 1) && (sl + 1) * kSlot <= nqb * P) p = sl * kSlot + (kSlot - 1 - (p - sl * kSlot));
+  }
+  const int blk = p / P, pair = p - blk * P;
+  const int qb = a.causal ? nqb - 1 - blk : blk;
+  const int b = pair / a.n_heads, hp = pair - b * a.n_heads;
+  const int group = a.n_heads / a.kv_heads;
+  const int kvh = hp % a.kv_heads, h = kvh * group + hp / a.kv_heads;
+  const int Sq = a.Sq, S = a.Sk, off = a.q_offset;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int l32 = lane & 31, h2 = lane >> 5;
+  const T* kbase = static_cast<const T*>(a.k.p) + b * a.k.batch + kvh * a.k.head;
+  const T* vbase = static_cast<const T*>(a.v.p) + b * a.v.batch + kvh * a.v.head;
+  const long long kld = a.k.token, vld = a.v.token;
+  const int32_t* mk = a.key_mask ? a.key_mask + static_cast<long long>(b) * S : nullptr;
+  const int32_t* kd = a.q_doc ? a.k_doc + static_cast<long long>(b) * S : nullptr;
+  const int qw0 = qb * QB + wave * 32;        // first query of this wavefront
+  const int qi = qw0 + l32;                   // this lane's query
+  const int qpos = qi + off;
+  const int pre = a.causal && a.prefix ? a.prefix[b] : 0;
+  const bool causal = a.causal;
+
+  vec qf[KS];
+  {
+    const int qc = qi < Sq ? qi : Sq - 1;
+    const T* qp = static_cast<const T*>(a.q.p) + b * a.q.batch + qc * a.q.token + h * a.q.head;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const vec*>(qp + 16 * ks + 8 * h2);
+  }
+  int kend = S;
+  if (causal) {
+    const int last = (qb + 1) * QB + off;
+    kend = last > pre ? last : pre;
+    kend = kend < S ? kend : S;
+  }
+  constexpr float kLog2e = 1.4426950408889634f;
+  const float c2 = CAP ? a.scores.scale * (2.f * kLog2e) / a.scores.softcap : a.scores.scale * kLog2e;
+  const float capc = a.scores.softcap * kLog2e;
+  const float slope2 = BIAS && a.scores.slopes ? a.scores.slopes[h] * kLog2e : 0.f;
+
+  // documents of the wavefront's queries: this lane's, and whether all are one
+  int qd = 0;
+  bool q_one = true;
+  if (kd) {
+    const int32_t* qds = a.q_doc + static_cast<long long>(b) * Sq;
+    qd = qds[qi < Sq ? qi : Sq - 1];
+    q_one = __ballot(qd != __builtin_amdgcn_readfirstlane(qd)) == 0;
+  }
+  const bool sparse = mk || kd;
+  if (sparse) {
+    int dmin = 0, dmax = 0;
+    if (kd) {
+      const int32_t* qds = a.q_doc + static_cast<long long>(b) * Sq;
+      const int i0 = qb * QB + lane, i1 = i0 + 64;
+      const int d0 = qds[i0 < Sq ? i0 : Sq - 1], d1 = qds[i1 < Sq ? i1 : Sq - 1];
+      dmin = d0 < d1 ? d0 : d1;
+      dmax = d0 < d1 ? d1 : d0;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const int x = __shfl_xor(dmin, o, 64), y = __shfl_xor(dmax, o, 64);
+        dmin = x < dmin ? x : dmin;
+        dmax = y > dmax ? y : dmax;
+      }
+    }
+    for (int i = threadIdx.x; i < kTileWords; i += 256) sTiles[i] = 0;
+    __syncthreads();
+    const int top = kend < kTileWords * 32 * KB ? kend : kTileWords * 32 * KB;
+    // 256 keys (4 tiles) a step, 4 keys a lane, 4 steps of loads in flight
+    for (int k0 = wave * 1024; k0 < top; k0 += NW * 1024) {
+      i32x4 m[4], d[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int key = k0 + 256 * u + 4 * lane;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[u][e] = d[u][e] = 0;
+        if (key + 4 <= S) {
+          if (mk) m[u] = *reinterpret_cast<const i32x4*>(mk + key);
+          if (kd) d[u] = *reinterpret_cast<const i32x4*>(kd + key);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (mk && key + e < S) m[u][e] = mk[key + e];
+            if (kd && key + e < S) d[u][e] = kd[key + e];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int key = k0 + 256 * u + 4 * lane;
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          any |= key + e < S && (!mk || m[u][e] != 0) && (!kd || (d[u][e] >= dmin && d[u][e] <= dmax));
+        const unsigned long long on = __ballot(any);
+        uint32_t four = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) four |= ((on >> (16 * t)) & 0xffffull ? 1u : 0u) << t;
+        const int tile0 = (k0 + 256 * u) / KB;
+        if (lane == 0 && four && tile0 < kTileWords * 32) atomicOr(&sTiles[tile0 / 32], four << (tile0 % 32));
+      }
+    }
+    __syncthreads();
+  }
+  // first key of the next tile to visit at or after t (a multiple of KB)
+  auto next_tile = [&](int t) {
+    if (!sparse) return t;
+    while (t < kend && t < kTileWords * 32 * KB) {
+      const int i = t / KB;
+      const uint32_t w = __builtin_amdgcn_readfirstlane(sTiles[i / 32]) >> (i % 32);
+      if (w) return t + KB * __builtin_ctz(w);
+      t = (i / 32 + 1) * 32 * KB;
+    }
+    return t;
+  };
+
+  float mrun = -INFINITY, lrun = 0.f;
+  f32x16 oacc[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[c][i] = 0.f;
+
+  // swizzles: chunk c of key row r sits at chunk position c ^ f(r) (k_flash)
+  const int cr = lane / CPR, cpos = lane % CPR;
+  int mraw = 1, draw = 0;                     // wavefront 0: mask and document of key kb + lane of the tile in flight
+  auto issue = [&](int kb, T* dk, T* dv) {
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+      const int r = (wave * LPW + j) * RPI + cr;
+      int key = kb + r;
+      key = key < S ? key : S - 1;
+      const int fk = (r / RPL) % CPR, fv = 4 * ((r / RPL) % (CPR / 4));
+      dma16(kbase + key * kld + 8 * (cpos ^ fk), dk + (wave * LPW + j) * RPI * HD);
+      dma16(vbase + key * vld + 8 * (cpos ^ fv), dv + (wave * LPW + j) * RPI * HD);
+    }
+    if (wave == 0 && sparse) {
+      const int key = kb + lane < S ? kb + lane : S - 1;
+      if (mk) mraw = mk[key];
+      if (kd) draw = kd[key];
+    }
+  };
+  const int kswz = (l32 / RPL) % CPR;
+  const int g = lane >> 4, e4 = (lane & 15) >> 2, q4 = lane & 3;
+  const int vrow = 4 * (g >> 1) + e4;
+  const int vswz4 = (vrow / RPL) % (CPR / 4);
+  const int vsub = 2 * (g & 1) + (q4 >> 1);
+  const int vin = 4 * (q4 & 1);
+  uint32_t vaddr[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) vaddr[c] = 2 * (vrow * HD + 8 * (4 * (c ^ vswz4) + vsub) + vin);
+
+  // one key tile from stage BUF (the other stage receives the tile at `next`)
+  auto tile = [&](auto BUF, int kb, int next) {
+    constexpr int buf = decltype(BUF)::value;
+    T* sk = buf ? sK1 : sK0;
+    T* sv = buf ? sV1 : sV0;
+    if (wave == 0 && sparse) {
+      const unsigned long long bits = __ballot(mraw != 0);
+      if (kd) sDoc[buf][lane] = draw;
+      const bool one = __ballot(draw != __builtin_amdgcn_readfirstlane(draw)) == 0;
+      if (lane == 0) {
+        sBits[buf] = bits;
+        sOne[buf] = one;
+      }
+    }
+    wait_vmcnt0();                              // this wavefront's copies of the tile landed
+    __syncthreads();
+    if (next < kend) issue(next, buf ? sK0 : sK1, buf ? sV0 : sV1);
+    // every key of the tile past this wavefront's queries and the prefix
+    if (causal && kb > qw0 + 31 + off && kb >= pre) return;
+    unsigned long long bits = S - kb >= KB ? ~0ull : (1ull << (S - kb)) - 1;
+    bool docs = kd != nullptr;
+    if (sparse) {
+      bits &= sBits[buf];
+      if (docs && q_one && sOne[buf]) {
+        if (__builtin_amdgcn_readfirstlane(sDoc[buf][0]) != __builtin_amdgcn_readfirstlane(qd)) return;
+        docs = false;
+      }
+    }
+    // ---- S^T = K Q^T: two 32-key blocks
+    f32x16 sacc[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sacc[kk][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const vec kf = *reinterpret_cast<const vec*>(sk + (32 * kk + l32) * HD + 8 * ((2 * ks + h2) ^ kswz));
+        sacc[kk] = Mfma32A<T>::run(kf, qf[ks], sacc[kk]);
+      }
+    }
+    // ---- scores in log2 units
+    if constexpr (CAP) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = __builtin_amdgcn_exp2f(sacc[kk][i] * c2) + 1.f;
+          sacc[kk][i] = fmaf(-2.f * capc, __builtin_amdgcn_rcpf(e), capc);
+        }
+    }
+    if constexpr (BIAS) {
+      const float dist = static_cast<float>(qpos - kb - 4 * h2);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = CAP ? sacc[kk][i] : sacc[kk][i] * c2;
+          sacc[kk][i] = fmaf(-slope2, fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))), x);
+        }
+    }
+    constexpr bool LOG2 = CAP || BIAS;          // already in log2 units
+    // ---- masks
+    const int last = qw0 + off > pre - 1 ? qw0 + off : pre - 1;
+    if (bits != ~0ull || docs || (causal && kb + KB - 1 > last)) {
+      unsigned long long vis = bits;
+      if (causal) {
+        // keys up to the query's own position or before the prefix
+        const int n = (qpos + 1 > pre ? qpos + 1 : pre) - kb;
+        vis &= n >= KB ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+      }
+      vis >>= 4 * h2;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          i32x4 kdoc;
+          if (docs) kdoc = *reinterpret_cast<const i32x4*>(&sDoc[buf][32 * kk + 8 * i4 + 4 * h2]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            bool ok = (vis >> (32 * kk + 8 * i4 + r)) & 1ull;
+            if (docs) ok = ok && kdoc[r] == qd;
+            sacc[kk][4 * i4 + r] = ok ? sacc[kk][4 * i4 + r] : -INFINITY;
+          }
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mt = LOG2 ? mx : mx * c2;
+    if (__ballot(mt > mrun + kTau)) {          // move the maximum (wavefront-uniform)
+      const float mnew = fmaxf(mrun, mt);
+      const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+      lrun *= alpha;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
+      mrun = mnew;
+    }
+    const float msub = mrun == -INFINITY ? 0.f : mrun;
+    // ---- probabilities, their sum, and P^T as 16-bit B operands
+    vec pb[4];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float s0 = sacc[kk][8 * hf + 2 * j], s1 = sacc[kk][8 * hf + 2 * j + 1];
+          const float p0 = __builtin_amdgcn_exp2f(LOG2 ? s0 - msub : fmaf(s0, c2, -msub));
+          const float p1 = __builtin_amdgcn_exp2f(LOG2 ? s1 - msub : fmaf(s1, c2, -msub));
+          lrun += p0 + p1;
+          w[j] = pack2<T>(p0, p1);
+        }
+        pb[2 * kk + hf] = __builtin_bit_cast(vec, w);
+      }
+    }
+    // ---- O^T += V^T P^T: four 16-key steps; the V^T operands of step
+    // k2 + 1 are read while step k2 multiplies
+    const uint32_t vb = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_vptr)sv));
+    u32x2 vf[2][CB][2];
+    auto vread = [&](auto K2, u32x2 (&dst)[CB][2]) {
+      constexpr int k2 = decltype(K2)::value;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        dst[c][0] = lds_read_tr16<(16 * k2) * HD * 2>(vb + vaddr[c]);
+        dst[c][1] = lds_read_tr16<(16 * k2 + 8) * HD * 2>(vb + vaddr[c]);
+      }
+    };
+    auto vmul = [&](int k2, u32x2 (&src)[CB][2]) {
+#pragma unroll
+      for (int c = 0; c < CB; ++c) {
+        u32x4 w;
+        w[0] = src[c][0][0]; w[1] = src[c][0][1]; w[2] = src[c][1][0]; w[3] = src[c][1][1];
+        oacc[c] = Mfma32A<T>::run(__builtin_bit_cast(vec, w), pb[k2], oacc[c]);
+      }
+    };
+    vread(std::integral_constant<int, 0>(), vf[0]);
+    vread(std::integral_constant<int, 1>(), vf[1]);
+    lgkm_wait<2 * CB>(&vf[0][0][0], 2 * CB);
+    vmul(0, vf[0]);
+    vread(std::integral_constant<int, 2>(), vf[0]);
+    lgkm_wait<2 * CB>(&vf[1][0][0], 2 * CB);
+    vmul(1, vf[1]);
+    vread(std::integral_constant<int, 3>(), vf[1]);
+    lgkm_wait<2 * CB>(&vf[0][0][0], 2 * CB);
+    vmul(2, vf[0]);
+    lgkm_wait<0>(&vf[1][0][0], 2 * CB);
+    vmul(3, vf[1]);
+  };
+  int kb = next_tile(0);
+  if (kb < kend) issue(kb, sK0, sV0);
+  while (kb < kend) {
+    const int n1 = next_tile(kb + KB);
+    tile(std::integral_constant<int, 0>(), kb, n1);
+    if (n1 >= kend) break;
+    kb = next_tile(n1 + KB);
+    tile(std::integral_constant<int, 1>(), n1, kb);
+  }
+  // ---- normalise and store: lane holds channels 32c + 8i + 4(lane/32) + r of its query
+  const float L = lrun + __shfl_xor(lrun, 32, 64);
+  float odd = 0.f * L;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) odd = fmaf(oacc[c][i], 0.f, odd);
+  const unsigned long long odd_lanes = __ballot(odd != 0.f);   // (NaN != 0)
+  uint32_t again = static_cast<uint32_t>(odd_lanes) | static_cast<uint32_t>(odd_lanes >> 32);
+  if (qi < Sq && !(again >> l32 & 1)) {
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    T* out = static_cast<T*>(a.out.p) + b * a.out.batch + qi * a.out.token + h * a.out.head;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u32x2 r2;
+        r2[0] = pack2<T>(oacc[c][4 * i] * inv, oacc[c][4 * i + 1] * inv);
+        r2[1] = pack2<T>(oacc[c][4 * i + 2] * inv, oacc[c][4 * i + 3] * inv);
+        *reinterpret_cast<u32x2*>(out + 32 * c + 8 * i + 4 * h2) = r2;
+      }
+  }
+  for (; __builtin_expect(again != 0, 0); again &= again - 1) {
+    const int i = qw0 + __builtin_ctz(again);
+    if (i < Sq) prompt_row<T, HD>(a, b, h, i);
+  }
+}
+
+template <typename T, int HD>
+void prompt_flash(const gm_prompt_attention& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.Sq + 127) / 128) * a.n_heads * a.B), block(256);
+  const bool cap = a.scores.softcap > 0.f;
+  // without a cap the maximum is taken before the scale, which has to keep its order
+  const bool bias = a.scores.slopes || (!cap && !(a.scores.scale > 0.f));
+  if (cap && bias) hipLaunchKernelGGL((k_prompt_flash<T, HD, true, true>), grid, block, 0, s, a);
+  else if (cap) hipLaunchKernelGGL((k_prompt_flash<T, HD, true, false>), grid, block, 0, s, a);
+  else if (bias) hipLaunchKernelGGL((k_prompt_flash<T, HD, false, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_prompt_flash<T, HD, false, false>), grid, block, 0, s, a);
+}
+
 }  // namespace
 
 void launch_attention_prompt(const gm_prompt_attention& a, hipStream_t s) {
   if (a.dtype == kF32) prompt_rows<float>(a, s);
-  else if (a.dtype == kBF16) prompt_rows<bf16_t>(a, s);
-  else prompt_rows<f16_t>(a, s);
+  else if (a.head_dim == 32) a.dtype == kBF16 ? prompt_rows<bf16_t>(a, s) : prompt_rows<f16_t>(a, s);
+  else if (a.dtype == kBF16) a.head_dim == 64 ? prompt_flash<bf16_t, 64>(a, s) : prompt_flash<bf16_t, 128>(a, s);
+  else a.head_dim == 64 ? prompt_flash<f16_t, 64>(a, s) : prompt_flash<f16_t, 128>(a, s);
 }
 
 }  // namespace gm
