@@ -398,7 +398,9 @@ void k_prompt_flash(gm_prompt_attention a) {
       for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
       mrun = mnew;
     }
-    const float msub = mrun == -INFINITY ? 0.f : mrun;
+    // fp16 probabilities times 2^7 (at most 2^15): fewer fall below its smallest normal
+    constexpr float kUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
+    const float msub = mrun == -INFINITY ? 0.f : mrun - kUp;
     // ---- probabilities, their sum, and P^T as 16-bit B operands
     vec pb[4];
 #pragma unroll

@@ -222,72 +222,119 @@ void launch_kv_read(const gm_kv_cache& c, int dtype, int B, int n, const int32_t
 }
 
 // ------------------------------------------------------------ attention over the cache
+//
+// The cache is read once per row block of queries by workgroups that take chunks of
+// the keys; each leaves, per query row, its largest score m (log2 units), the sum l
+// of its exp2(score - m) and its own normalised output o, and the chunks of a row
+// are merged as sum(w o) / sum(w), w = l exp2(m - largest m), in their order.
 namespace {
 
-// Key chunks per sequence and key head: chunk s of sequence b covers keys
-// [s, s + 1) * ceil(length / nsplit), rounded up to whole tiles of 64.
-int cached_splits(const gm_kv_cache& c, int B, int Sq, int n_heads) {
-  const long long rows = static_cast<long long>(B) * Sq * n_heads;
-  long long want = (1024 + rows - 1) / rows;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Row r of key head kvh of sequence b: token r / G, query head kvh * G + r % G.
+struct CachedPlan {
+  int rows;         // query rows of a key head: Sq * (n_heads / heads)
+  int blocks;       // row blocks of a key head
+  int nsplit;       // key chunks per row block
+};
+
+// The MFMA kernel takes 16-bit dtypes: 16 columns of a product are shared by query
+// rows and 32-channel groups.  In fp32 a workgroup takes one row.
+CachedPlan cached_plan(const gm_kv_cache& c, int dtype, int B, int Sq, int n_heads) {
+  CachedPlan p;
+  p.rows = Sq * (n_heads / c.heads);
+  const int per_block = dtype == kF32 ? 1 : 16 / (c.head_dim / kKvGroup);
+  p.blocks = (p.rows + per_block - 1) / per_block;
+  const long long wgs = static_cast<long long>(B) * c.heads * p.blocks;
+  long long want = (1024 + wgs - 1) / wgs;
   const long long most = (c.max_seq + 255) / 256;
   want = want < most ? want : most;
-  return static_cast<int>(want < 64 ? want : 64);
+  p.nsplit = static_cast<int>(want < 64 ? want : 64);
+  return p;
 }
 
-// Workgroup = one query row (sequence, token, head) and one chunk of its keys.
-// HD / 8 lanes hold a key row, 8 channels each; every lane group keeps an
-// online softmax of its own, merged by shuffles and in LDS.  With one chunk the
-// workgroup writes the output, else (m, l, o) to the workspace.
+// What a workgroup works on: sequence, key head, row block and its chunk of the
+// keys [k0, k1) of a sequence of len keys, whole tiles of 64.
+struct CachedPlace {
+  int b, kvh, blk, split, len, k0, k1;
+  __device__ __forceinline__ CachedPlace(const gm_cached_attention& a, const gm_kv_cache& c,
+                                         const CachedPlan& p) {
+    int x = blockIdx.x;
+    blk = x % p.blocks;
+    x /= p.blocks;
+    kvh = x % c.heads;
+    b = x / c.heads;
+    split = blockIdx.y;
+    len = a.lengths[b];
+    len = len < c.max_seq ? len : c.max_seq;
+    len = len > 0 ? len : 0;
+    const int per = (len + 64 * p.nsplit - 1) / (64 * p.nsplit) * 64;
+    k0 = split * per;
+    k1 = k0 + per < len ? k0 + per : len;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ T* cached_out(const gm_cached_attention& a, const gm_kv_cache& c, int b,
+                                         int kvh, int r) {
+  const int G = a.n_heads / c.heads;
+  return static_cast<T*>(a.out.p) + b * a.out.batch + (r / G) * a.out.token +
+         (kvh * G + r % G) * a.out.head;
+}
+// (m, l, o[HD]) of a chunk
+template <int HD>
+__device__ __forceinline__ float* cached_part(const gm_cached_attention& a, const gm_kv_cache& c,
+                                              const CachedPlan& p, int b, int kvh, int r, int split) {
+  const long long row = (static_cast<long long>(b) * c.heads + kvh) * p.rows + r;
+  return static_cast<float*>(a.workspace) + (row * p.nsplit + split) * (HD + 2);
+}
+
+// One query row by a workgroup.  HD / 8 lanes hold a key row, 8 channels each; every
+// lane group keeps an online softmax of its own, merged by shuffles and in LDS.
 template <typename T, int HD, int BITS>
 __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_kv_cache c,
-                                                     int nsplit) {
+                                                     CachedPlan plan) {
   constexpr int OFF = 1 << (BITS - 1), NWV = 4;
   constexpr int G = HD / 8, KPW = 64 / G, NG = NWV * KPW;
   __shared__ float s_m[NWV], s_l[NWV], s_o[NWV][HD];
-  const int row = blockIdx.x, split = blockIdx.y;
-  const int h = row % a.n_heads, i = row / a.n_heads % a.Sq, b = row / a.n_heads / a.Sq;
-  const int kvh = h / (a.n_heads / c.heads);
+  const CachedPlace w(a, c, plan);
+  const int GQ = a.n_heads / c.heads, i = w.blk / GQ, h = w.kvh * GQ + w.blk % GQ;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int grp = lane / G, gl = lane % G;
-  int len = a.lengths[b];
-  len = len < c.max_seq ? len : c.max_seq;
-  const int qpos = len - a.Sq + i;
-  const int per = len > 0 ? (len + 64 * nsplit - 1) / (64 * nsplit) * 64 : 0;
-  const int k0 = split * per;
-  int k1 = k0 + per;
-  k1 = k1 < qpos + 1 ? k1 : qpos + 1;
+  const int qpos = w.len - a.Sq + i;
+  const int k1 = w.k1 < qpos + 1 ? w.k1 : qpos + 1;
   const float slope = a.scores.slopes ? a.scores.slopes[h] : 0.f;
   float q[8];
   {
     Row8<T> r;
-    r.load(static_cast<const T*>(a.q.p) + b * a.q.batch + i * a.q.token + h * a.q.head + 8 * gl);
+    r.load(static_cast<const T*>(a.q.p) + w.b * a.q.batch + i * a.q.token + h * a.q.head + 8 * gl);
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = r.get(j);
   }
-  const long long head = static_cast<long long>(b) * c.heads + kvh;
+  const long long head = static_cast<long long>(w.b) * c.heads + w.kvh;
   const char* kc = static_cast<const char*>(c.k) + head * c.max_seq * (HD * BITS / 8) + gl * BITS;
   const char* vc = static_cast<const char*>(c.v) + head * c.max_seq * (HD * BITS / 8) + gl * BITS;
   const long long sbase = (head * (HD / kKvGroup) + gl / 4) * c.max_seq;
   const uint16_t* ks = static_cast<const uint16_t*>(c.k_scale) + sbase;
   const uint16_t* vs = static_cast<const uint16_t*>(c.v_scale) + sbase;
-  const uint8_t* valid = c.valid ? c.valid + static_cast<long long>(b) * c.max_seq : nullptr;
+  const uint8_t* valid = c.valid ? c.valid + static_cast<long long>(w.b) * c.max_seq : nullptr;
   auto codes = [&](const char* p, float (&x)[8]) {
     if constexpr (BITS == 8) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        x[j] = static_cast<float>(static_cast<int>((w[j / 4] >> (8 * (j % 4))) & 255u) - OFF);
+        x[j] = static_cast<float>(static_cast<int>((v[j / 4] >> (8 * (j % 4))) & 255u) - OFF);
     } else {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        x[j] = static_cast<float>(static_cast<int>((w >> (4 * j)) & 15u) - OFF);
+        x[j] = static_cast<float>(static_cast<int>((v >> (4 * j)) & 15u) - OFF);
     }
   };
   float m = -INFINITY, l = 0.f, o[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) o[j] = 0.f;
-  for (int key = k0 + wave * KPW + grp; key < k1; key += NG) {
+  for (int key = w.k0 + wave * KPW + grp; key < k1; key += NG) {
     float kx[8], vx[8];
     codes(kc + static_cast<long long>(key) * (HD * BITS / 8), kx);
     codes(vc + static_cast<long long>(key) * (HD * BITS / 8), vx);
@@ -330,65 +377,383 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
   const int ch = threadIdx.x;
   if (ch >= HD) return;
   float M = -INFINITY, L = 0.f, O = 0.f;
-  for (int w = 0; w < NWV; ++w) M = fmaxf(M, s_m[w]);
-  for (int w = 0; w < NWV; ++w) {
-    const float f = s_m[w] == -INFINITY ? 0.f : expf(s_m[w] - M);
-    L += s_l[w] * f;
-    O += s_o[w][ch] * f;
+  for (int x = 0; x < NWV; ++x) M = fmaxf(M, s_m[x]);
+  for (int x = 0; x < NWV; ++x) {
+    const float f = s_m[x] == -INFINITY ? 0.f : expf(s_m[x] - M);
+    L += s_l[x] * f;
+    O += s_o[x][ch] * f;
   }
-  if (nsplit == 1) {
-    T* out = static_cast<T*>(a.out.p) + b * a.out.batch + i * a.out.token + h * a.out.head;
-    out[ch] = from_f32<T>(L == 0.f ? 0.f : O / L);
+  O = L == 0.f ? 0.f : O / L;
+  if (plan.nsplit == 1) {
+    cached_out<T>(a, c, w.b, w.kvh, w.blk)[ch] = from_f32<T>(O);
     return;
   }
-  float* part = static_cast<float*>(a.workspace) +
-                (static_cast<long long>(row) * nsplit + split) * (HD + 2);
+  float* part = cached_part<HD>(a, c, plan, w.b, w.kvh, w.blk, w.split);
   part[2 + ch] = O;
   if (ch == 0) {
-    part[0] = M;
+    part[0] = M * kLog2e;
     part[1] = L;
+  }
+}
+
+// ------------------------------------------------------------ 16-bit: MFMA
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Sum over the NG lanes n that share a row (they hold its groups), in each of them.
+template <int NG>
+__device__ __forceinline__ float group_sum(float v) {
+  if constexpr (NG >= 2)
+    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0xB1, 0xf, 0xf, true));
+  if constexpr (NG == 4)
+    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x4E, 0xf, 0xf, true));
+  return v;
+}
+
+// BYTES bytes as 32-bit words (a lone byte or half word zero-extended).
+template <int BYTES>
+__device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
+  if constexpr (BYTES == 1) w[0] = *reinterpret_cast<const uint8_t*>(p);
+  else if constexpr (BYTES == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
+  else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+  else if constexpr (BYTES == 8) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+    w[0] = v[0];
+    w[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < BYTES / 16; ++i) {
+      const u32x4 v = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+    }
+  }
+}
+
+// Workgroup = one row block of a key head and one chunk of the keys, its 4 wavefronts
+// taking tiles of 32 keys in turn; no LDS and no barrier before the end.  Codes become
+// fp16 operands of v_mfma_f32_16x16x32 by bit operations alone: code bits in the
+// low bits of an fp16 are the subnormal code * 2^-24 (bits 4-7: 16 code * 2^-24), which
+// the instruction multiplies exactly.  Columns n of a product = (query row n / NG, channel group n % NG), NG = HD / 32:
+//  S[key][n]: A = K codes, lane (key row m, lane / 16 = g) holding HD / 4 consecutive
+//    channels, which lie in one group; B = the query, zero outside the column's group; the
+//    codes' offset 2^(BITS - 1) is taken off the sums' start.  So
+//    a lane has the sums of its group for 8 keys, multiplies by the group's K scales and
+//    adds the NG lanes of its row.  Rows 4 g + r of product u are keys 8 g + 4 u + r.
+//  O[ch][n] += V codes * w, the codes' offset taken off them first (a packed fp16 addition,
+//    exact; taken off the sums it would leave errors of an offset times w), w = exp2(score - m) * V scale of the column's group, rounded to
+//    fp16 after division by a power of two kept within 8 of the scales met and times 16 (at
+//    most 2^15: what is rounded below the smallest normal is 2^-26 of the largest).  The 8 keys whose
+//    scores a lane holds are the 8 k slots of its B operand, so w needs no exchange; A row m
+//    of product i is channel (HD / 16) m + i, a lane reading HD / 16 channels of 8 keys.
+//    A lane's own column counts where the channel's group is the column's.
+// The query is divided by a power of two as well (largest element to 2^14), so that bf16
+// and fp16 rows become fp16 without loss.  The maximum m moves lazily (by more than 2^8).
+template <typename T, int HD, int BITS, bool CAP>
+__global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_kv_cache c,
+                                                     CachedPlan plan) {
+  constexpr int OFF = 1 << (BITS - 1), NWV = 4, KB = 32;
+  constexpr int NG = HD / kKvGroup, RB = 16 / NG;   // groups, rows per block
+  constexpr int KD = HD * BITS / 128;               // words of a lane's K chunk
+  constexpr int VB = HD * BITS / 128, VD = VB < 4 ? 1 : VB / 4;   // bytes, words of its V chunk
+  constexpr int NI = HD / 16;                       // products of O
+  constexpr float kTau = 8.f, kTiny = 1.f / 16777216.f;           // 2^-24
+  __shared__ float s_m[NWV][RB], s_l[NWV][RB], s_o[NWV][RB][HD + 1];
+  const CachedPlace w(a, c, plan);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = lane & 15, g = lane >> 4, t = n % NG;
+  const int r = w.blk * RB + n / NG;                // this column's query row
+  const bool row_ok = r < plan.rows;
+  const int GQ = a.n_heads / c.heads, rr = row_ok ? r : 0, i = rr / GQ, h = w.kvh * GQ + rr % GQ;
+  const int qpos = row_ok ? w.len - a.Sq + i : -1;
+  const float slope2 = a.scores.slopes ? a.scores.slopes[h] * kLog2e : 0.f;
+
+  // ---- the query as B operands: k step st, slots 2 d and 2 d + 1 hold the channels whose
+  // codes the unpacking below puts there
+  f16x8 qf[NG];
+  float c0, up;                                     // start of the sums of S; half of their unit
+  float c2 = CAP ? a.scores.scale * (2.f * kLog2e) / a.scores.softcap : a.scores.scale * kLog2e;
+  {
+    constexpr int NC = HD / 4;
+    float x[NC], big = 0.f, sum = 0.f;
+    const T* q = static_cast<const T*>(a.q.p) + w.b * a.q.batch + i * a.q.token + h * a.q.head + NC * g;
+#pragma unroll
+    for (int j = 0; j < NC / 8; ++j) {
+      Row8<T> v;
+      v.load(q + 8 * j);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[8 * j + e] = v.get(e);
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j) big = fmaxf(big, fabsf(x[j]));
+    big = fmaxf(big, __shfl_xor(big, 16, 64));
+    big = fmaxf(big, __shfl_xor(big, 32, 64));
+    const int ex = big > 0.f && big < INFINITY ? static_cast<int>(__float_as_uint(big) >> 23) - 127 : 0;
+    const bool mine = t == g * NG / 4;
+#pragma unroll
+    for (int st = 0; st < NG; ++st)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        // slot j of word j / 2: nibbles j / 2 and j / 2 + 4, or bytes j
+        const int ch = BITS == 4 ? j / 2 + 4 * (j % 2) : j;
+        const float v = mine ? ldexpf(x[8 * st + ch], 14 - ex) : 0.f;
+        const float sixteen = BITS == 4 && (j / 2) % 2 ? 0.0625f : 1.f;
+        const _Float16 f = static_cast<_Float16>(v * sixteen);
+        qf[st][j] = f;
+        sum += static_cast<float>(f) * (1.f / sixteen);
+      }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    c0 = -static_cast<float>(OFF) * kTiny * sum;
+    // the sums' unit 2^24 / 2^(14 - ex) in two factors, each far from the ends of fp32
+    up = ldexpf(1.f, (10 + ex) / 2);
+    c2 = ldexpf(c2, 10 + ex - (10 + ex) / 2);
+  }
+  const float capc = a.scores.softcap * kLog2e;
+
+  const long long head = static_cast<long long>(w.b) * c.heads + w.kvh;
+  const char* kc = static_cast<const char*>(c.k) + head * c.max_seq * (HD * BITS / 8) +
+                   (8 * (n >> 2) + (n & 3)) * (HD * BITS / 8) + 4 * KD * g;
+  const char* vc = static_cast<const char*>(c.v) + head * c.max_seq * (HD * BITS / 8) +
+                   8 * g * (HD * BITS / 8) + VB * n;
+  const uint16_t* ks = static_cast<const uint16_t*>(c.k_scale) + (head * NG + t) * c.max_seq + 8 * g;
+  const uint16_t* vs = static_cast<const uint16_t*>(c.v_scale) + (head * NG + t) * c.max_seq + 8 * g;
+  const uint8_t* valid = c.valid ? c.valid + static_cast<long long>(w.b) * c.max_seq + 8 * g : nullptr;
+
+  struct Tile {
+    uint32_t k[2][KD], v[8][VD];
+    u32x4 ks, vs;
+    u32x2 valid;
+  } cur;
+  auto fetch = [&](int kb, Tile& x) {
+    const long long row = static_cast<long long>(kb) * (HD * BITS / 8);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) load_words<4 * KD>(kc + row + 4 * u * (HD * BITS / 8), x.k[u]);
+    x.ks = *reinterpret_cast<const u32x4*>(ks + kb);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) load_words<VB>(vc + row + j * (HD * BITS / 8), x.v[j]);
+    x.vs = *reinterpret_cast<const u32x4*>(vs + kb);
+    if (valid) x.valid = *reinterpret_cast<const u32x2*>(valid + kb);
+  };
+
+  float m = -INFINITY, l = 0.f;
+  float bound = 0.f, inv_bound = 0.f;               // power of two at or above the V scales met
+  f32x4 o[NI];
+#pragma unroll
+  for (int e = 0; e < NI; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f16x8 off[2];                                     // the codes' offset, in units of 2^-24 and 2^-20
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    off[0][j] = static_cast<_Float16>(OFF * kTiny);
+    off[1][j] = static_cast<_Float16>(OFF * kTiny * (BITS == 4 ? 16.f : 1.f));
+  }
+
+  int kb = w.k0 + KB * wave;
+  if (kb < w.k1) fetch(kb, cur);
+  for (; kb < w.k1; kb += NWV * KB) {
+    Tile x = cur;
+    if (kb + NWV * KB < w.k1) fetch(kb + NWV * KB, cur);
+    // ---- scores of 8 keys
+    float s[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4 acc = {c0, c0, c0, c0};
+#pragma unroll
+      for (int st = 0; st < NG; ++st) {
+        u32x4 f;
+        if constexpr (BITS == 4) {
+          const uint32_t lo = x.k[u][st], hi = lo >> 8;
+          f[0] = lo & 0x000f000fu;
+          f[1] = lo & 0x00f000f0u;
+          f[2] = hi & 0x000f000fu;
+          f[3] = hi & 0x00f000f0u;
+        } else {
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            f[d] = __builtin_amdgcn_perm(0u, x.k[u][2 * st + d / 2], d % 2 ? 0x0c030c02u : 0x0c010c00u);
+        }
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, f), qf[st], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[4 * u + e] = acc[e];
+    }
+    float top = -INFINITY;
+    const float dist = static_cast<float>(qpos - kb - 8 * g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float sk = bf16_value(j % 2 ? x.ks[j / 2] >> 16 : x.ks[j / 2] & 0xffffu);
+      float y = group_sum<NG>(s[j] * (sk * up)) * c2;
+      if constexpr (CAP) y = fmaf(-2.f * capc, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f), capc);
+      y = fmaf(-slope2, dist - static_cast<float>(j), y);
+      bool ok = kb + 8 * g + j <= qpos && kb + 8 * g + j < w.k1;
+      if (valid) ok = ok && ((x.valid[j / 4] >> (8 * (j % 4))) & 255u) != 0;
+      s[j] = ok ? y : -INFINITY;
+      top = fmaxf(top, s[j]);
+    }
+    if (__ballot(top > m + kTau)) {
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float mn = fmaxf(m, top);
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < NI; ++e) o[e] *= f;
+      m = mn;
+    }
+    // ---- V scales; hidden keys' are 0 (they may be NaN)
+    float sv[8], most = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      sv[j] = bf16_value(j % 2 ? x.vs[j / 2] >> 16 : x.vs[j / 2] & 0xffffu);
+      sv[j] = s[j] == -INFINITY ? 0.f : sv[j];
+      most = fmaxf(most, sv[j]);
+    }
+    if (__ballot(most > 8.f * bound)) {
+      most = fmaxf(most, __shfl_xor(most, 16, 64));
+      most = fmaxf(most, __shfl_xor(most, 32, 64));
+      const uint32_t e = __float_as_uint(most) >> 23;
+      // 2^(e + 1 - 127), its reciprocal a normal number
+      float b = __uint_as_float((e < 2 ? 2 : e > 252 ? 253 : e + 1) << 23);
+      b = most > 8.f * bound ? b : bound;
+      const float ib = __uint_as_float((254u << 23) - __float_as_uint(b));
+      const float f = bound > 0.f ? bound * ib : 0.f;
+#pragma unroll
+      for (int e2 = 0; e2 < NI; ++e2) o[e2] *= f;
+      bound = b;
+      inv_bound = ib;
+    }
+    // ---- weights
+    const float msub = m == -INFINITY ? 0.f : m;
+    f16x8 wf;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float p = __builtin_amdgcn_exp2f(s[j] - msub);
+      l += p;
+      wf[j] = static_cast<_Float16>(p * (sv[j] * (16.f * inv_bound)));
+    }
+    // ---- O += V w: word j of product e holds keys 2 j (low half) and 2 j + 1
+    if constexpr (BITS == 4) {
+#pragma unroll
+      for (int half = 0; half < (NI + 3) / 4; ++half) {
+        u32x4 lo, hi;                               // 4 channels of 8 keys, and shifted down by two
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          lo[j] = __builtin_amdgcn_perm(x.v[2 * j + 1][0], x.v[2 * j][0], half ? 0x07060302u : 0x05040100u);
+          hi[j] = lo[j] >> 8;
+        }
+#pragma unroll
+        for (int e = 0; e < (NI < 4 ? NI : 4); ++e) {
+          u32x4 f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = (e < 2 ? lo[j] : hi[j]) & (e % 2 ? 0x00f000f0u : 0x000f000fu);
+          o[4 * half + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              __builtin_bit_cast(f16x8, f) - off[e % 2], wf, o[4 * half + e], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < NI; ++e) {
+        u32x4 f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          f[j] = __builtin_amdgcn_perm(x.v[2 * j + 1][e / 4], x.v[2 * j][e / 4],
+                                       0x0c040c00u + 0x00010001u * (e % 4));
+        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, f) - off[0], wf, o[e], 0, 0, 0);
+      }
+    }
+  }
+  // ---- the wavefront's normalised output: rows 4 g + e of product x are channels
+  // NI (4 g + e) + x, of group g NG / 4
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (t == g * NG / 4) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int x = 0; x < NI; ++x) {
+        const float unit = BITS == 4 && x % 2 ? 65536.f : 1048576.f;   // 2^20 or 2^24, over 16
+        s_o[wave][n / NG][NI * (4 * g + e) + x] =
+            l == 0.f ? 0.f : (o[x][e] * unit * inv) * bound;
+      }
+  }
+  if (t == 0 && g == 0) {
+    s_m[wave][n / NG] = m;
+    s_l[wave][n / NG] = l;
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < RB * HD; e += 256) {
+    const int ch = e % HD, row = e / HD, gr = w.blk * RB + row;
+    if (gr >= plan.rows) break;
+    float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll
+    for (int x = 0; x < NWV; ++x) M = fmaxf(M, s_m[x][row]);
+#pragma unroll
+    for (int x = 0; x < NWV; ++x) {
+      const float f = s_m[x][row] == -INFINITY && s_l[x][row] == 0.f
+                          ? 0.f : s_l[x][row] * __builtin_amdgcn_exp2f(s_m[x][row] - M);
+      L += f;
+      O += f == 0.f ? 0.f : f * s_o[x][row][ch];
+    }
+    O = L == 0.f ? 0.f : O / L;
+    if (plan.nsplit == 1) {
+      cached_out<T>(a, c, w.b, w.kvh, gr)[ch] = from_f32<T>(O);
+    } else {
+      float* part = cached_part<HD>(a, c, plan, w.b, w.kvh, gr, w.split);
+      part[2 + ch] = O;
+      if (ch == 0) {
+        part[0] = M;
+        part[1] = L;
+      }
+    }
   }
 }
 
 // The chunks of a row merged in their order.
 template <typename T, int HD>
-__global__ __launch_bounds__(HD) void k_cached_merge(gm_cached_attention a, int nsplit) {
-  const int row = blockIdx.x, ch = threadIdx.x;
-  const int h = row % a.n_heads, i = row / a.n_heads % a.Sq, b = row / a.n_heads / a.Sq;
-  const float* part = static_cast<const float*>(a.workspace) +
-                      static_cast<long long>(row) * nsplit * (HD + 2);
+__global__ __launch_bounds__(HD) void k_cached_merge(gm_cached_attention a, gm_kv_cache c,
+                                                     CachedPlan plan) {
+  const int ch = threadIdx.x;
+  int x = blockIdx.x;
+  const int r = x % plan.rows;
+  x /= plan.rows;
+  const int kvh = x % c.heads, b = x / c.heads;
+  const float* part = cached_part<HD>(a, c, plan, b, kvh, r, 0);
   float M = -INFINITY, L = 0.f, O = 0.f;
-  for (int s = 0; s < nsplit; ++s) M = fmaxf(M, part[s * (HD + 2)]);
-  for (int s = 0; s < nsplit; ++s) {
-    const float ms = part[s * (HD + 2)];
-    const float f = ms == -INFINITY ? 0.f : expf(ms - M);
-    L += part[s * (HD + 2) + 1] * f;
-    O += part[s * (HD + 2) + 2 + ch] * f;
+  for (int s = 0; s < plan.nsplit; ++s) M = fmaxf(M, part[s * (HD + 2)]);
+  for (int s = 0; s < plan.nsplit; ++s) {
+    const float ms = part[s * (HD + 2)], ls = part[s * (HD + 2) + 1];
+    const float f = ls == 0.f ? 0.f : ls * __builtin_amdgcn_exp2f(ms - M);
+    L += f;
+    O += f == 0.f ? 0.f : f * part[s * (HD + 2) + 2 + ch];
   }
-  T* out = static_cast<T*>(a.out.p) + b * a.out.batch + i * a.out.token + h * a.out.head;
-  out[ch] = from_f32<T>(L == 0.f ? 0.f : O / L);
+  cached_out<T>(a, c, b, kvh, r)[ch] = from_f32<T>(L == 0.f ? 0.f : O / L);
 }
 
 }  // namespace
 
-uint64_t attention_cached_workspace(const gm_kv_cache& c, int, int B, int Sq, int n_heads) {
-  if (B == 0 || Sq == 0) return 0;
-  const int nsplit = cached_splits(c, B, Sq, n_heads);
-  if (nsplit == 1) return 0;
-  return static_cast<uint64_t>(B) * Sq * n_heads * nsplit * (c.head_dim + 2) * sizeof(float);
+uint64_t attention_cached_workspace(const gm_kv_cache& c, int dtype, int B, int Sq, int n_heads) {
+  const CachedPlan p = cached_plan(c, dtype, B, Sq, n_heads);
+  if (p.nsplit == 1) return 0;
+  return static_cast<uint64_t>(B) * c.heads * p.rows * p.nsplit * (c.head_dim + 2) * sizeof(float);
 }
 
 void launch_attention_cached(const gm_cached_attention& a, hipStream_t s) {
   const gm_kv_cache& c = *a.cache;
-  const int nsplit = cached_splits(c, a.B, a.Sq, a.n_heads);
-  const unsigned rows = static_cast<unsigned>(a.B) * a.Sq * a.n_heads;
+  const CachedPlan p = cached_plan(c, a.dtype, a.B, a.Sq, a.n_heads);
+  const unsigned heads = static_cast<unsigned>(a.B) * c.heads;
+  const dim3 grid(heads * p.blocks, p.nsplit), block(256);
   by_cache(a.dtype, c, [&](auto t, auto hd, auto bits) {
     typedef decltype(t) T;
-    constexpr int HD = decltype(hd)::value;
-    hipLaunchKernelGGL((k_cached_rows<T, HD, decltype(bits)::value>), dim3(rows, nsplit), dim3(256),
-                       0, s, a, c, nsplit);
-    if (nsplit > 1)
-      hipLaunchKernelGGL((k_cached_merge<T, HD>), dim3(rows), dim3(HD), 0, s, a, nsplit);
+    constexpr int HD = decltype(hd)::value, BITS = decltype(bits)::value;
+    if constexpr (std::is_same<T, float>::value)
+      hipLaunchKernelGGL((k_cached_rows<T, HD, BITS>), grid, block, 0, s, a, c, p);
+    else if (a.scores.softcap > 0.f)
+      hipLaunchKernelGGL((k_cached_mfma<T, HD, BITS, true>), grid, block, 0, s, a, c, p);
+    else
+      hipLaunchKernelGGL((k_cached_mfma<T, HD, BITS, false>), grid, block, 0, s, a, c, p);
+    if (p.nsplit > 1)
+      hipLaunchKernelGGL((k_cached_merge<T, HD>), dim3(heads * p.rows), dim3(HD), 0, s, a, c, p);
   });
 }
 

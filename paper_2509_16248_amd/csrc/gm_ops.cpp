@@ -128,7 +128,9 @@ int gm_kv_read(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n, co
 
 uint64_t gm_attention_cached_workspace(const gm_kv_cache* cache, int32_t dtype, int32_t B,
                                        int32_t Sq, int32_t n_heads) {
-  if (check_cache(cache) || check_dtype(dtype) || B < 1 || Sq < 1 || n_heads < 1) return 0;
+  if (check_cache(cache) || check_dtype(dtype) || B < 1 || Sq < 1 || n_heads < 1 ||
+      n_heads % cache->heads)
+    return 0;
   return attention_cached_workspace(*cache, dtype, B, Sq, n_heads);
 }
 

@@ -26,7 +26,7 @@ def stored(x, bits):
     return (q.unflatten(-1, (-1, GROUP)) * s.unsqueeze(-1)).flatten(-2)
 
 
-def attention(q, k, v, visible, distance, scale, softcap=0.0, slopes=None, tol=None):
+def attention(q, k, v, visible, distance, scale, softcap=0.0, slopes=None, tol=None, floor=0.0):
     """q [Sq, H, hd], k and v [Sk, Hkv, hd], visible and distance [Sq, Sk] -> float64
     [Sq, H, hd].  Hidden keys are left out, not multiplied by zero.
 
@@ -37,7 +37,9 @@ def attention(q, k, v, visible, distance, scale, softcap=0.0, slopes=None, tol=N
     to the dtype, and (2 e + (2 n + 16) 2^-24) w for p and the sums: a score's fp32
     dot product of hd terms, cap, bias and exponent argument are off by at most
     (hd + 16) 2^-24 (scale sum |q_c k_c| + |bias|) + 2^-20 softcap, an exponential
-    by 2^-22, and the sums of n weights and of n products by n 2^-24 each."""
+    by 2^-22, and the sums of n weights and of n products by n 2^-24 each.  ``floor``:
+    what a weight loses at the most in the subnormals of fp16, relative to the largest
+    weight (their sum is at least 1) times the largest value."""
     fi = torch.finfo(q.dtype)
     u = fi.eps / 2
     q, k, v = (t.detach().cpu().double() for t in (q, k, v))
@@ -68,7 +70,11 @@ def attention(q, k, v, visible, distance, scale, softcap=0.0, slopes=None, tol=N
             size = torch.where(visible & torch.isfinite(size), size, 0.0).amax(-1, keepdim=True)
             e = (hd + 16) * 2.0 ** -24 * size + 2.0 ** -20 * softcap
             w = torch.nan_to_num(p[:, ~bad]) @ vv[~bad].abs()
-            tol[:, h] = u * o.abs() + u * fi.tiny + (u + 2 * e + (2 * k.shape[0] + 16) * 2.0 ** -24) * w
+            n = k.shape[0]
+            seen = visible.any(0) & ~bad
+            largest = vv[seen].abs().max() if seen.any() else 0.0
+            tol[:, h] = (u * o.abs() + u * fi.tiny + n * floor * largest
+                         + (u + 2 * e + (2 * n + 16) * 2.0 ** -24) * w)
     return out
 
 
@@ -90,8 +96,10 @@ def prompt(q, k, v, causal=False, softcap=0.0, slopes=None, key_mask=None, q_doc
             vis = vis & (key_mask[b].cpu() != 0)[None]
         if q_doc is not None:
             vis = vis & (q_doc[b].cpu()[:, None] == k_doc[b].cpu()[None])
+        # fp16 probabilities are held times 2^7: half a step of the subnormals is 2^-32
         out[b] = attention(q[b], k[b], v[b], vis, (i - j).abs(), scale, softcap, slopes,
-                           None if tol is None else tol[b])
+                           None if tol is None else tol[b],
+                           2.0 ** -32 if q.dtype == torch.float16 else 0.0)
     return out
 
 
@@ -107,8 +115,13 @@ def cached(q, k, v, lengths, bits, softcap=0.0, slopes=None, valid=None, scale=N
         vis = j <= i
         if valid is not None:
             vis = vis & (valid[b].cpu() != 0)[None]
+        # 16-bit dtypes: a weight is p times a value's scale, in fp16 as 16 / b of itself with
+        # b at most twice the largest scale s; half a step of the subnormals, 2^-25, stands for
+        # 2^-25 b / 16 <= 2^-28 s, times a code of at most Q: 2^-28 of the largest value
+        # (which may be Q s (1 - 2^-8) by the rounding of s)
         out[b] = attention(q[b], ks[b], vs[b], vis, (i - j).abs(), scale, softcap, slopes,
-                           None if tol is None else tol[b])
+                           None if tol is None else tol[b],
+                           0.0 if q.dtype == torch.float32 else 2.0 ** -28 * (1 + 2.0 ** -7))
     return out
 
 
