@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -25,68 +26,70 @@ _DTYPES = {torch.float32: gm.GM_DTYPE_F32, torch.bfloat16: gm.GM_DTYPE_BF16,
            torch.float16: gm.GM_DTYPE_F16}
 
 
-def _rows(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype, device) -> gm.gm_tensor:
-    if t.dim() != 4 or tuple(t.shape) != tuple(shape):
+# The arguments as the C structs lay them out, packed in one go: filling nested
+# ctypes structures field by field takes longer than a small kernel runs.
+_CACHED = struct.Struct("@P4i" + 2 * "P3q" + "P" + "2fP" + "PQ")
+_PROMPT = struct.Struct("@7i" + 4 * "P3q" + "2i" + "2fP" + "4P")
+_TENSOR = struct.Struct("@P3q")
+assert _CACHED.size == ctypes.sizeof(gm.gm_cached_attention)
+assert _PROMPT.size == ctypes.sizeof(gm.gm_prompt_attention)
+assert _TENSOR.size == ctypes.sizeof(gm.gm_tensor)
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> Tuple[int, int, int, int]:
+    """The fields of a gm_tensor."""
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}, not {t.device}")
-    if t.numel() and t.stride(3) != 1:
+    batch, token, head, channel = t.stride()
+    if channel != 1 and t.numel():
         raise ValueError(f"the channels of {name} must be contiguous")
-    return gm.gm_tensor(t.data_ptr() or None, t.stride(0), t.stride(1), t.stride(2))
+    return t.data_ptr(), batch, token, head
 
 
 def _ints(t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], device,
-          dtype=torch.int32) -> Optional[int]:
+          dtype=torch.int32) -> int:
+    """Address of a small array, 0 for none."""
     if t is None:
-        return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        return 0
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}, not {t.device}")
-    return t.data_ptr() or None
+    return t.data_ptr()
 
 
 def _first(t: torch.Tensor, name: str):
-    """(dtype, device) of a call, by its first tensor."""
-    if t.dtype not in _DTYPES:
+    """(dtype, its gm code, device) of a call, by its first tensor."""
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, not {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a HIP device, not {t.device}")
-    return t.dtype, t.device
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [batch, tokens, heads, head_dim]")
+    return t.dtype, code, t.device
 
 
-def _scores(scale: Optional[float], softcap: float, slopes: Optional[torch.Tensor], heads: int,
-            head_dim: int, device) -> gm.gm_scores:
-    return gm.gm_scores(1.0 / math.sqrt(head_dim) if scale is None else scale, softcap,
-                        _ints(slopes, "slopes", (heads,), device, torch.float32))
-
-
-class _On:
-    """The device and the stream of a call, and the tensors it uses."""
-
-    def __init__(self, device, stream):
-        if stream is not None and stream.device != device:
-            raise ValueError(f"the stream must be on {device}, not {stream.device}")
-        self.given = stream is not None
-        self.stream = stream if self.given else torch.cuda.current_stream(device)
-        self.context = torch.cuda.stream(self.stream)   # also makes its device current
-
-    def __enter__(self):
-        self.context.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        return self.context.__exit__(*exc)
-
-    def uses(self, *tensors):
-        """On a stream given by the caller the allocator has to know that the
-        tensors are in use there."""
-        if self.given:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+def _on(device, stream, call, tensors):
+    """call(stream handle) with the device current; on a stream given by the
+    caller, what the call allocates belongs to that stream, and the allocator
+    is told that the tensors are in use there."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream(device).cuda_stream)
+    if stream is None:
+        with torch.cuda.device(device):
+            return call(torch.cuda.current_stream(device).cuda_stream)
+    if stream.device != device:
+        raise ValueError(f"the stream must be on {device}, not {stream.device}")
+    with torch.cuda.stream(stream):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        return call(stream.cuda_stream)
 
 
 class KvCache:
@@ -139,15 +142,20 @@ class KvCache:
         cache are not stored.  ``mask`` int32 [B, n]: 0 hides a position from
         attention (a ``masked`` cache; without it every stored position may be
         attended)."""
-        dtype, device = _first(k, "k")
-        B, n = self._shape(k, device)
+        dtype, code, device = _first(k, "k")
+        B, n = k.shape[0], k.shape[1]
+        if device != self.device:
+            raise ValueError(f"the cache is on {self.device}, the rows on {device}")
+        if B > self.batch:
+            raise ValueError(f"the rows' batch {B} exceeds the cache's {self.batch}")
         shape = (B, n, self.heads, self.head_dim)
-        kt, vt = (_rows(t, name, shape, dtype, device) for t, name in ((k, "k"), (v, "v")))
-        with _On(device, stream) as on:
-            on.uses(k, v, start, count, mask, *self._tensors())
-            gm.gm_kv_write(self.c, _DTYPES[dtype], B, n, kt, vt,
-                           _ints(start, "start", (B,), device), _ints(count, "count", (B,), device),
-                           _ints(mask, "mask", (B, n), device), on.stream.cuda_stream)
+        kt, vt = (gm.gm_tensor.from_buffer_copy(_TENSOR.pack(*_rows(t, name, shape, dtype, device)))
+                  for t, name in ((k, "k"), (v, "v")))
+        st, ct = _ints(start, "start", (B,), device), _ints(count, "count", (B,), device)
+        mt = _ints(mask, "mask", (B, n), device)
+        _on(device, stream,
+            lambda s: gm.gm_kv_write(self.c, code, B, n, kt, vt, st, ct, mt, s),
+            (k, v, start, count, mask, *self._tensors()))
 
     def read(self, n: int, start: Optional[torch.Tensor] = None,
              count: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
@@ -159,28 +167,26 @@ class KvCache:
         into; ``batch``: the first B sequences (default: all)."""
         if out is not None:
             dtype = out[0].dtype
-        if dtype not in _DTYPES:
+        code = _DTYPES.get(dtype)
+        if code is None:
             raise ValueError(f"dtype must be float32, bfloat16 or float16, not {dtype}")
         B = self.batch if batch is None else batch
         if not 0 <= B <= self.batch or n < 0:
             raise ValueError("batch must be at most the cache's, and n not negative")
-        shape = (B, n, self.heads, self.head_dim)
-        with _On(self.device, stream) as on:
-            if out is None:
-                out = tuple(torch.empty(shape, dtype=dtype, device=self.device) for _ in "kv")
-            kt, vt = (_rows(t, name, shape, dtype, self.device)
-                      for t, name in zip(out, ("k", "v")))
-            on.uses(start, count, *out, *self._tensors())
-            gm.gm_kv_read(self.c, _DTYPES[dtype], B, n, _ints(start, "start", (B,), self.device),
-                          _ints(count, "count", (B,), self.device), kt, vt, on.stream.cuda_stream)
-        return tuple(out)
+        shape, device = (B, n, self.heads, self.head_dim), self.device
+        st, ct = _ints(start, "start", (B,), device), _ints(count, "count", (B,), device)
 
-    def _shape(self, t: torch.Tensor, device) -> Tuple[int, int]:
-        if device != self.device:
-            raise ValueError(f"the cache is on {self.device}, the rows on {device}")
-        if t.dim() != 4 or t.shape[0] > self.batch:
-            raise ValueError("rows must be [B, n, heads, head_dim] with B at most the cache's batch")
-        return t.shape[0], t.shape[1]
+        def call(s):
+            k, v = out if out is not None else (
+                torch.empty(shape, dtype=dtype, device=device),
+                torch.empty(shape, dtype=dtype, device=device))
+            kt, vt = (gm.gm_tensor.from_buffer_copy(
+                _TENSOR.pack(*_rows(t, name, shape, dtype, device)))
+                for t, name in ((k, "k"), (v, "v")))
+            gm.gm_kv_read(self.c, code, B, n, st, ct, kt, vt, s)
+            return k, v
+
+        return _on(device, stream, call, (start, count, *(out or ()), *self._tensors()))
 
 
 def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
@@ -196,29 +202,30 @@ def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
     ``scale`` (default 1/sqrt(head_dim)) times q.k, capped as softcap *
     tanh(score / softcap) when softcap > 0, less slopes[h] * distance
     (``slopes`` float32 [n_heads])."""
-    dtype, device = _first(q, "q")
-    if q.dim() != 4 or q.shape[0] > cache.batch or device != cache.device:
-        raise ValueError("q must be [B, Sq, n_heads, head_dim] on the cache's device, with B at "
-                         "most the cache's batch")
-    B, Sq, H, hd = q.shape
-    if hd != cache.head_dim:
-        raise ValueError(f"q must have the cache's head_dim {cache.head_dim}, not {hd}")
+    dtype, code, device = _first(q, "q")
+    shape = q.shape
+    B, Sq, H, hd = shape
+    if device != cache.device or B > cache.batch or hd != cache.head_dim:
+        raise ValueError(f"q must be on the cache's device {cache.device}, with at most its "
+                         f"{cache.batch} sequences and its head_dim {cache.head_dim}")
     if lengths is None:
         raise ValueError("lengths is missing")
-    with _On(device, stream) as on:
-        if out is None:
-            out = torch.empty((B, Sq, H, hd), dtype=dtype, device=device)
-        need = gm.gm_attention_cached_workspace(cache.c, _DTYPES[dtype], B, Sq, H)
+    qt, lt = _rows(q, "q", shape, dtype, device), _ints(lengths, "lengths", (B,), device)
+    sl = _ints(slopes, "slopes", (H,), device, torch.float32)
+    need = gm.gm_attention_cached_workspace(cache.c, code, B, Sq, H)
+
+    def call(s):
+        res = torch.empty(shape, dtype=dtype, device=device) if out is None else out
         work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        a = gm.gm_cached_attention(
-            ctypes.pointer(cache.c), _DTYPES[dtype], B, Sq, H,
-            _rows(q, "q", q.shape, dtype, device), _rows(out, "out", q.shape, dtype, device),
-            _ints(lengths, "lengths", (B,), device),
-            _scores(scale, softcap, slopes, H, hd, device),
-            work.data_ptr() if need else None, need)
-        on.uses(q, out, lengths, slopes, *cache._tensors())
-        gm.gm_attention_cached(a, on.stream.cuda_stream)
-    return out
+        a = gm.gm_cached_attention.from_buffer_copy(_CACHED.pack(
+            ctypes.addressof(cache.c), code, B, Sq, H, *qt,
+            *_rows(res, "out", shape, dtype, device), lt,
+            1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl,
+            work.data_ptr() if need else 0, need))
+        gm.gm_attention_cached(a, s)
+        return res
+
+    return _on(device, stream, call, (q, out, lengths, slopes, *cache._tensors()))
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False,
@@ -236,23 +243,25 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool
     past the query or lies before ``prefix`` [B] (all int32, each optional); a
     query that sees nothing gives zeros.  Scores as in
     :func:`cached_attention`."""
-    dtype, device = _first(q, "q")
-    if q.dim() != 4 or k.dim() != 4:
-        raise ValueError("q and k must be [batch, tokens, heads, head_dim]")
-    B, Sq, H, hd = q.shape
+    dtype, code, device = _first(q, "q")
+    _first(k, "k")
+    qs = q.shape
+    B, Sq, H, hd = qs
     Sk, Hkv = k.shape[1], k.shape[2]
-    shape = (B, Sk, Hkv, hd)
-    with _On(device, stream) as on:
-        if out is None:
-            out = torch.empty((B, Sq, H, hd), dtype=dtype, device=device)
-        a = gm.gm_prompt_attention(
-            _DTYPES[dtype], B, Sq, Sk, H, Hkv, hd, _rows(q, "q", q.shape, dtype, device),
-            _rows(k, "k", shape, dtype, device), _rows(v, "v", shape, dtype, device),
-            _rows(out, "out", q.shape, dtype, device), int(causal),
-            Sk - Sq if q_offset is None else q_offset,
-            _scores(scale, softcap, slopes, H, hd, device),
-            _ints(key_mask, "key_mask", (B, Sk), device), _ints(q_doc, "q_doc", (B, Sq), device),
-            _ints(k_doc, "k_doc", (B, Sk), device), _ints(prefix, "prefix", (B,), device))
-        on.uses(q, k, v, out, slopes, key_mask, q_doc, k_doc, prefix)
-        gm.gm_attention(a, on.stream.cuda_stream)
-    return out
+    ks = (B, Sk, Hkv, hd)
+    qt, kt, vt = (_rows(q, "q", qs, dtype, device), _rows(k, "k", ks, dtype, device),
+                  _rows(v, "v", ks, dtype, device))
+    sl = _ints(slopes, "slopes", (H,), device, torch.float32)
+    masks = (_ints(key_mask, "key_mask", (B, Sk), device), _ints(q_doc, "q_doc", (B, Sq), device),
+             _ints(k_doc, "k_doc", (B, Sk), device), _ints(prefix, "prefix", (B,), device))
+
+    def call(s):
+        res = torch.empty(qs, dtype=dtype, device=device) if out is None else out
+        a = gm.gm_prompt_attention.from_buffer_copy(_PROMPT.pack(
+            code, B, Sq, Sk, H, Hkv, hd, *qt, *kt, *vt, *_rows(res, "out", qs, dtype, device),
+            bool(causal), Sk - Sq if q_offset is None else q_offset,
+            1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl, *masks))
+        gm.gm_attention(a, s)
+        return res
+
+    return _on(device, stream, call, (q, k, v, out, slopes, key_mask, q_doc, k_doc, prefix))
