@@ -45,137 +45,196 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   return v > w ? v : w;
 }
 
-// x / s rounded to the nearest integer, ties to even, limited to [-Q, Q].  The
-// quotient by the hardware reciprocal is off by one at most; x - q s is exact
-// in fp32 (s has 8 significant bits, q 7, and the difference is no larger than
-// s / 2 or so), so comparing it with s / 2 settles the nearest integer.
-template <int Q>
-__device__ __forceinline__ int quantise(float x, float s, float inv) {
-  float q = rintf(x * inv);
-  const float r = fmaf(-q, s, x), half = 0.5f * s;
-  const float a = fabsf(r);
-  const bool odd = static_cast<int>(q) & 1;
-  if (a > half || (a == half && odd)) q += r > 0.f ? 1.f : -1.f;
-  return static_cast<int>(fminf(fmaxf(q, -static_cast<float>(Q)), static_cast<float>(Q)));
+// 8 channels' bits without their signs, the largest in each half of the word (16-bit
+// types; Inf and NaN are the largest) or the largest (fp32).
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                __builtin_bit_cast(u16x2, b)));
 }
+template <typename T>
+__device__ __forceinline__ uint32_t largest_bits(const Row8<T>& row) {
+  uint32_t m = 0;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t u = row.raw[i / 4][i % 4] & 0x7fffffffu;
+      m = u > m ? u : m;
+    }
+    return quad_max(m);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max_u16x2(m, row.raw[0][i] & 0x7fff7fffu);
+    m = m >> 16 > (m & 0xffffu) ? m >> 16 : m & 0xffffu;
+    m = quad_max(m);
+    return __float_as_uint(to_f32(__builtin_bit_cast(T, static_cast<uint16_t>(m))));
+  }
+}
+
+// x / s rounded to the nearest integer (ties to even), limited to [-Q, Q], plus
+// 2^(BITS - 1), in the low byte of the result (the bytes above are not 0).  The
+// quotient is refined once, to 2^-45 of itself before it is rounded to fp32, and
+// that settles the integer: a quotient on a half k + 1/2 is an fp32 number and
+// comes out exact, and any other of a 24-bit x and an 8-bit s lies more than
+// (1 + 2^-8) half steps of fp32 away from one.  Adding 1.5 2^23 rounds it.
+template <int BITS>
+__device__ __forceinline__ uint32_t quantise(float x, float s, float inv) {
+  constexpr float Q = BITS == 8 ? 127.f : 7.f, kRound = 12582912.f + (1 << (BITS - 1));
+  float q = x * inv;
+  q = fmaf(fmaf(-q, s, x), inv, q);
+  return __float_as_uint(__builtin_amdgcn_fmed3f(q, -Q, Q) + kRound);
+}
+// Bytes 0 of four words.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u),
+                               __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
+// x / d and x % d of 32-bit numbers by one multiplication: m = ceil(2^(32 + s) / d) less
+// 2^32, 2^s >= d.
+struct Div {
+  uint32_t d, m, s;
+  Div() = default;
+  explicit Div(uint32_t divisor) : d(divisor), s(0) {
+    while (s < 32 && (1ull << s) < d) ++s;
+    m = static_cast<uint32_t>(((1ull << 32) * ((1ull << s) - d)) / d + 1);
+  }
+  __device__ __forceinline__ uint32_t div(uint32_t x, uint32_t& rest) const {
+    const uint32_t t = __umulhi(m, x);
+    const uint32_t q = s ? (t + ((x - t) >> 1)) >> (s - 1) : x;
+    rest = x - q * d;
+    return q;
+  }
+};
 
 struct KvRows {
   gm_kv_cache c;
   gm_tensor k, v;
   const int32_t *start, *count, *mask;
   int B, n;
+  Div by_n, by_heads;
 };
 
-// Which row and channels a thread handles: 8 channels `ch` of head h of row i of
+// Which row and channels an item is: 8 channels `ch` of head h of row i of
 // sequence b, of k or v.  Channels run fastest, then the rows of a head, whose
 // codes are contiguous in the cache.
 struct KvPlace {
   int b, i, h, which, ch, pos;
+  bool some;      // there is such a row
   bool live;      // row within its count and position within the cache
 };
 template <int HD>
-__device__ __forceinline__ bool kv_place(const KvRows& a, KvPlace& p) {
+__device__ __forceinline__ KvPlace kv_place(const KvRows& a, uint64_t e) {
   constexpr int C8 = HD / 8;
-  const uint64_t e = blockIdx.x * 256ull + threadIdx.x;
+  KvPlace p;
+  const uint32_t x = static_cast<uint32_t>(e / C8);   // (a launch has fewer than 2^32 items)
+  uint32_t i, h;
   p.ch = static_cast<int>(e % C8) * 8;
-  uint64_t r = e / C8;
-  p.i = static_cast<int>(r % a.n);
-  r /= a.n;
+  const uint32_t r = a.by_n.div(x, i);
+  p.i = static_cast<int>(i);
   p.which = static_cast<int>(r & 1);
-  r >>= 1;
-  p.h = static_cast<int>(r % a.c.heads);
-  r /= a.c.heads;
-  if (r >= static_cast<uint64_t>(a.B)) return false;
-  p.b = static_cast<int>(r);
+  const uint32_t b = a.by_heads.div(r >> 1, h);
+  p.h = static_cast<int>(h);
+  p.some = b < static_cast<uint32_t>(a.B);
+  p.b = p.some ? static_cast<int>(b) : 0;
   const long long pos = static_cast<long long>(a.start ? a.start[p.b] : 0) + p.i;
-  p.live = pos >= 0 && pos < a.c.max_seq && (!a.count || p.i < a.count[p.b]);
+  p.live = p.some && pos >= 0 && pos < a.c.max_seq && (!a.count || p.i < a.count[p.b]);
   p.pos = p.live ? static_cast<int>(pos) : 0;
-  return true;
+  return p;
+}
+template <int HD, int BITS>
+__device__ __forceinline__ char* kv_codes(const KvRows& a, const KvPlace& p) {
+  const long long head = static_cast<long long>(p.b) * a.c.heads + p.h;
+  return static_cast<char*>(p.which ? a.c.v : a.c.k) +
+         (head * a.c.max_seq + p.pos) * (HD * BITS / 8) + p.ch * BITS / 8;
+}
+template <int HD>
+__device__ __forceinline__ uint16_t* kv_scale(const KvRows& a, const KvPlace& p) {
+  const long long head = static_cast<long long>(p.b) * a.c.heads + p.h;
+  return static_cast<uint16_t*>(p.which ? a.c.v_scale : a.c.k_scale) +
+         (head * (HD / kKvGroup) + p.ch / kKvGroup) * a.c.max_seq + p.pos;
+}
+template <typename T>
+__device__ __forceinline__ T* kv_row(const KvRows& a, const KvPlace& p) {
+  const gm_tensor& t = p.which ? a.v : a.k;
+  return static_cast<T*>(t.p) + p.b * t.batch + p.i * t.token + p.h * t.head + p.ch;
 }
 
-// One thread per 8 channels of a row, 4 threads (a quad of lanes) per group.
-// The threads of a quad take the same branches: they share their row.
-template <typename T, int HD, int BITS>
+// A thread takes U items of 8 channels, 256 apart, their loads up front; 4 threads
+// (a quad of lanes) share a group, and with it their row and their branches.
+template <typename T, int HD, int BITS, int U>
 __global__ __launch_bounds__(256) void k_kv_write(KvRows a) {
   constexpr int Q = BITS == 8 ? 127 : 7, OFF = 1 << (BITS - 1);
-  KvPlace p;
-  if (!kv_place<HD>(a, p) || !p.live) return;
-  const gm_tensor& src = p.which ? a.v : a.k;
-  Row8<T> row;
-  row.load(static_cast<const T*>(src.p) + p.b * src.batch + p.i * src.token + p.h * src.head + p.ch);
-  float x[8];
-  uint32_t amax = 0;
+  KvPlace place[U];
+  Row8<T> rows[U];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    x[j] = row.get(j);
-    const uint32_t u = __float_as_uint(x[j]) & 0x7fffffffu;
-    amax = u > amax ? u : amax;
+  for (int u = 0; u < U; ++u) {
+    place[u] = kv_place<HD>(a, (static_cast<uint64_t>(blockIdx.x) * U + u) * 256 + threadIdx.x);
+    if (place[u].live) rows[u].load(kv_row<const T>(a, place[u]));
   }
-  amax = quad_max(amax);
-  const bool finite = amax < 0x7f800000u;
-  const uint32_t sb = finite ? bf16_bits(__uint_as_float(amax) * (1.0f / Q)) : 0x7fc0u;
-  // a scale whose reciprocal would overflow, or whose half be inexact: both
-  // sides of the quotient times 2^64 (exact)
-  const float up = amax < (40u << 23) ? 18446744073709551616.f : 1.f;
-  const float s = bf16_value(sb) * up;
-  const bool zero = !finite || s == 0.f;
-  const float inv = zero ? 0.f : __builtin_amdgcn_rcpf(s);
-  uint32_t code[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    code[j] = static_cast<uint32_t>((zero ? 0 : quantise<Q>(x[j] * up, s, inv)) + OFF);
-  const long long head = static_cast<long long>(p.b) * a.c.heads + p.h;
-  char* codes = static_cast<char*>(p.which ? a.c.v : a.c.k) +
-                (head * a.c.max_seq + p.pos) * (HD * BITS / 8) + p.ch * BITS / 8;
-  if constexpr (BITS == 8) {
-    u32x2 w;
-    w[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-    w[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
-    *reinterpret_cast<u32x2*>(codes) = w;
-  } else {
-    uint32_t w = 0;
+  for (int u = 0; u < U; ++u) {
+    const KvPlace& p = place[u];
+    if (!p.live) continue;
+    const uint32_t amax = largest_bits(rows[u]);
+    const bool finite = amax < 0x7f800000u;
+    const uint32_t sb = finite ? bf16_bits(__uint_as_float(amax) * (1.0f / Q)) : 0x7fc0u;
+    // a scale whose reciprocal would overflow: both sides of the quotient times 2^64
+    const float up = amax < (40u << 23) ? 18446744073709551616.f : 1.f;
+    const float s = bf16_value(sb) * up;
+    const bool zero = !finite || s == 0.f;
+    const float inv = zero ? 0.f : __builtin_amdgcn_rcpf(s);
+    uint32_t code[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w |= code[j] << (4 * j);
-    *reinterpret_cast<uint32_t*>(codes) = w;
+    for (int j = 0; j < 8; ++j) code[j] = zero ? OFF : quantise<BITS>(rows[u].get(j) * up, s, inv);
+    char* codes = kv_codes<HD, BITS>(a, p);
+    if constexpr (BITS == 8) {
+      u32x2 w;
+      w[0] = low_bytes(code[0], code[1], code[2], code[3]);
+      w[1] = low_bytes(code[4], code[5], code[6], code[7]);
+      *reinterpret_cast<u32x2*>(codes) = w;
+    } else {
+      *reinterpret_cast<uint32_t*>(codes) = low_bytes(code[0], code[2], code[4], code[6]) |
+                                            low_bytes(code[1], code[3], code[5], code[7]) << 4;
+    }
+    if (p.ch % kKvGroup == 0) *kv_scale<HD>(a, p) = static_cast<uint16_t>(sb);
+    if (a.c.valid && p.h == 0 && p.which == 0 && p.ch == 0)
+      a.c.valid[static_cast<long long>(p.b) * a.c.max_seq + p.pos] =
+          !a.mask || a.mask[static_cast<long long>(p.b) * a.n + p.i] != 0;
   }
-  if (p.ch % kKvGroup == 0) {
-    uint16_t* sc = static_cast<uint16_t*>(p.which ? a.c.v_scale : a.c.k_scale);
-    sc[(head * (HD / kKvGroup) + p.ch / kKvGroup) * a.c.max_seq + p.pos] = static_cast<uint16_t>(sb);
-  }
-  if (a.c.valid && p.h == 0 && p.which == 0 && p.ch == 0)
-    a.c.valid[static_cast<long long>(p.b) * a.c.max_seq + p.pos] =
-        !a.mask || a.mask[static_cast<long long>(p.b) * a.n + p.i] != 0;
 }
 
-template <typename T, int HD, int BITS>
+template <typename T, int HD, int BITS, int U>
 __global__ __launch_bounds__(256) void k_kv_read(KvRows a) {
   constexpr int OFF = 1 << (BITS - 1);
-  KvPlace p;
-  if (!kv_place<HD>(a, p)) return;
-  Row8<T> row;
-  if (p.live) {
-    const long long head = static_cast<long long>(p.b) * a.c.heads + p.h;
-    const char* codes = static_cast<const char*>(p.which ? a.c.v : a.c.k) +
-                        (head * a.c.max_seq + p.pos) * (HD * BITS / 8) + p.ch * BITS / 8;
-    const uint16_t* sc = static_cast<const uint16_t*>(p.which ? a.c.v_scale : a.c.k_scale);
-    const float s = bf16_value(sc[(head * (HD / kKvGroup) + p.ch / kKvGroup) * a.c.max_seq + p.pos]);
-    if constexpr (BITS == 8) {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(codes);
+  KvPlace place[U];
+  u32x2 w[U];
+  uint16_t sb[U];
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        row.set(j, static_cast<float>(static_cast<int>((w[j / 4] >> (8 * (j % 4))) & 255u) - OFF) * s);
-    } else {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(codes);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        row.set(j, static_cast<float>(static_cast<int>((w >> (4 * j)) & 15u) - OFF) * s);
+  for (int u = 0; u < U; ++u) {
+    place[u] = kv_place<HD>(a, (static_cast<uint64_t>(blockIdx.x) * U + u) * 256 + threadIdx.x);
+    w[u] = u32x2{0, 0};
+    sb[u] = 0;
+    if (place[u].live) {
+      const char* codes = kv_codes<HD, BITS>(a, place[u]);
+      if constexpr (BITS == 8) w[u] = *reinterpret_cast<const u32x2*>(codes);
+      else w[u][0] = *reinterpret_cast<const uint32_t*>(codes);
+      sb[u] = *kv_scale<HD>(a, place[u]);
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) row.set(j, 0.f);
   }
-  const gm_tensor& dst = p.which ? a.v : a.k;
-  row.store(static_cast<T*>(dst.p) + p.b * dst.batch + p.i * dst.token + p.h * dst.head + p.ch);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (!place[u].some) continue;
+    const float s = bf16_value(sb[u]);
+    Row8<T> row;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t code = BITS == 8 ? (w[u][j / 4] >> (8 * (j % 4))) & 255u : (w[u][0] >> (4 * j)) & 15u;
+      // (code - OFF) s, which fp32 holds exactly; rows that are not there have s = 0
+      row.set(j, fmaf(static_cast<float>(code), s, -OFF * s));
+    }
+    row.store(kv_row<T>(a, place[u]));
+  }
 }
 
 // f(storage type, head size, bits) with the three as compile-time values.
@@ -195,9 +254,13 @@ void by_cache(int dtype, const gm_kv_cache& c, F f) {
   else head(f16_t());
 }
 
-uint32_t kv_blocks(const KvRows& a) {
-  return static_cast<uint32_t>(
-      (static_cast<uint64_t>(a.B) * a.n * a.c.heads * 2 * (a.c.head_dim / 8) + 255) / 256);
+// f(items per thread, grid): one where there are few, so that they spread over the GPU.
+template <typename F>
+void kv_launch(const KvRows& a, F f) {
+  const uint64_t items = static_cast<uint64_t>(a.B) * a.n * a.c.heads * 2 * (a.c.head_dim / 8);
+  auto blocks = [&](int u) { return dim3(static_cast<uint32_t>((items + 256 * u - 1) / (256 * u))); };
+  if (items >= 256 * 4 * 2048) f(std::integral_constant<int, 4>(), blocks(4));
+  else f(std::integral_constant<int, 1>(), blocks(1));
 }
 
 }  // namespace
@@ -205,19 +268,23 @@ uint32_t kv_blocks(const KvRows& a) {
 void launch_kv_write(const gm_kv_cache& c, int dtype, int B, int n, const gm_tensor& k,
                      const gm_tensor& v, const int32_t* start, const int32_t* count,
                      const int32_t* mask, hipStream_t s) {
-  const KvRows a{c, k, v, start, count, mask, B, n};
-  by_cache(dtype, c, [&](auto t, auto hd, auto bits) {
-    hipLaunchKernelGGL((k_kv_write<decltype(t), decltype(hd)::value, decltype(bits)::value>),
-                       dim3(kv_blocks(a)), dim3(256), 0, s, a);
+  const KvRows a{c, k, v, start, count, mask, B, n, Div(n), Div(c.heads)};
+  kv_launch(a, [&](auto u, dim3 grid) {
+    by_cache(dtype, c, [&](auto t, auto hd, auto bits) {
+      hipLaunchKernelGGL((k_kv_write<decltype(t), decltype(hd)::value, decltype(bits)::value, decltype(u)::value>),
+                         grid, dim3(256), 0, s, a);
+    });
   });
 }
 
 void launch_kv_read(const gm_kv_cache& c, int dtype, int B, int n, const int32_t* start,
                     const int32_t* count, const gm_tensor& k, const gm_tensor& v, hipStream_t s) {
-  const KvRows a{c, k, v, start, count, nullptr, B, n};
-  by_cache(dtype, c, [&](auto t, auto hd, auto bits) {
-    hipLaunchKernelGGL((k_kv_read<decltype(t), decltype(hd)::value, decltype(bits)::value>),
-                       dim3(kv_blocks(a)), dim3(256), 0, s, a);
+  const KvRows a{c, k, v, start, count, nullptr, B, n, Div(n), Div(c.heads)};
+  kv_launch(a, [&](auto u, dim3 grid) {
+    by_cache(dtype, c, [&](auto t, auto hd, auto bits) {
+      hipLaunchKernelGGL((k_kv_read<decltype(t), decltype(hd)::value, decltype(bits)::value, decltype(u)::value>),
+                         grid, dim3(256), 0, s, a);
+    });
   });
 }
 
