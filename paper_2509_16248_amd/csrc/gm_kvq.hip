@@ -20,9 +20,9 @@ template <typename T> struct Row8 {
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = reinterpret_cast<const u32x4*>(p)[i];
   }
-  __device__ __forceinline__ void store(T* p) const {
+  __device__ __forceinline__ void store(T* p) const {   // past the caches: read back elsewhere, if at all
 #pragma unroll
-    for (int i = 0; i < NV; ++i) reinterpret_cast<u32x4*>(p)[i] = raw[i];
+    for (int i = 0; i < NV; ++i) __builtin_nontemporal_store(raw[i], reinterpret_cast<u32x4*>(p) + i);
   }
   __device__ __forceinline__ float get(int i) const { return to_f32(reinterpret_cast<const T*>(raw)[i]); }
   __device__ __forceinline__ void set(int i, float x) { reinterpret_cast<T*>(raw)[i] = from_f32<T>(x); }
@@ -94,7 +94,7 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 // 2^32, 2^s >= d.
 struct Div {
   uint32_t d, m, s;
-  Div() = default;
+  Div() : d(1), m(0), s(0) {}
   explicit Div(uint32_t divisor) : d(divisor), s(0) {
     while (s < 32 && (1ull << s) < d) ++s;
     m = static_cast<uint32_t>(((1ull << 32) * ((1ull << s) - d)) / d + 1);
@@ -112,7 +112,7 @@ struct KvRows {
   gm_tensor k, v;
   const int32_t *start, *count, *mask;
   int B, n;
-  Div by_n, by_heads;
+  Div by_n, by_heads, by_blocks;
 };
 
 // Which row and channels an item is: 8 channels `ch` of head h of row i of
@@ -123,20 +123,35 @@ struct KvPlace {
   bool some;      // there is such a row
   bool live;      // row within its count and position within the cache
 };
-template <int HD>
-__device__ __forceinline__ KvPlace kv_place(const KvRows& a, uint64_t e) {
-  constexpr int C8 = HD / 8;
+// Item u of a thread.  U = 1: items of every head in one line.  U > 1: a workgroup's
+// 256 U items are of one head, so that all but row and channel is the same for all of
+// its threads and stays in scalar registers.
+template <int HD, int U>
+__device__ __forceinline__ KvPlace kv_place(const KvRows& a, int u) {
+  constexpr uint32_t C8 = HD / 8;
   KvPlace p;
-  const uint32_t x = static_cast<uint32_t>(e / C8);   // (a launch has fewer than 2^32 items)
-  uint32_t i, h;
-  p.ch = static_cast<int>(e % C8) * 8;
-  const uint32_t r = a.by_n.div(x, i);
+  uint32_t i, h, r;
+  if constexpr (U == 1) {
+    const uint64_t e = blockIdx.x * 256ull + threadIdx.x;
+    p.ch = static_cast<int>(e % C8) * 8;
+    r = a.by_n.div(static_cast<uint32_t>(e / C8), i);   // (a launch has fewer than 2^32 items)
+  } else {
+    uint32_t blk;
+    r = __builtin_amdgcn_readfirstlane(a.by_blocks.div(blockIdx.x, blk));
+    const uint32_t e = (blk * U + u) * 256 + threadIdx.x;
+    p.ch = static_cast<int>(e % C8) * 8;
+    i = e / C8;
+  }
   p.i = static_cast<int>(i);
   p.which = static_cast<int>(r & 1);
-  const uint32_t b = a.by_heads.div(r >> 1, h);
+  uint32_t b = a.by_heads.div(r >> 1, h);
+  if constexpr (U > 1) {
+    b = __builtin_amdgcn_readfirstlane(b);
+    h = __builtin_amdgcn_readfirstlane(h);
+  }
   p.h = static_cast<int>(h);
-  p.some = b < static_cast<uint32_t>(a.B);
-  p.b = p.some ? static_cast<int>(b) : 0;
+  p.some = b < static_cast<uint32_t>(a.B) && i < static_cast<uint32_t>(a.n);
+  p.b = b < static_cast<uint32_t>(a.B) ? static_cast<int>(b) : 0;
   const long long pos = static_cast<long long>(a.start ? a.start[p.b] : 0) + p.i;
   p.live = p.some && pos >= 0 && pos < a.c.max_seq && (!a.count || p.i < a.count[p.b]);
   p.pos = p.live ? static_cast<int>(pos) : 0;
@@ -164,12 +179,12 @@ __device__ __forceinline__ T* kv_row(const KvRows& a, const KvPlace& p) {
 // (a quad of lanes) share a group, and with it their row and their branches.
 template <typename T, int HD, int BITS, int U>
 __global__ __launch_bounds__(256) void k_kv_write(KvRows a) {
-  constexpr int Q = BITS == 8 ? 127 : 7, OFF = 1 << (BITS - 1);
+  constexpr int Q = BITS == 8 ? 127 : 7;
   KvPlace place[U];
   Row8<T> rows[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    place[u] = kv_place<HD>(a, (static_cast<uint64_t>(blockIdx.x) * U + u) * 256 + threadIdx.x);
+    place[u] = kv_place<HD, U>(a, u);
     if (place[u].live) rows[u].load(kv_row<const T>(a, place[u]));
   }
 #pragma unroll
@@ -179,14 +194,19 @@ __global__ __launch_bounds__(256) void k_kv_write(KvRows a) {
     const uint32_t amax = largest_bits(rows[u]);
     const bool finite = amax < 0x7f800000u;
     const uint32_t sb = finite ? bf16_bits(__uint_as_float(amax) * (1.0f / Q)) : 0x7fc0u;
-    // a scale whose reciprocal would overflow: both sides of the quotient times 2^64
-    const float up = amax < (40u << 23) ? 18446744073709551616.f : 1.f;
-    const float s = bf16_value(sb) * up;
-    const bool zero = !finite || s == 0.f;
-    const float inv = zero ? 0.f : __builtin_amdgcn_rcpf(s);
+    float x[8], s = bf16_value(sb);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = rows[u].get(j);
+    if (__builtin_expect(amax < (40u << 23), 0)) {
+      // a scale whose reciprocal would overflow: both sides of the quotient times 2^64
+      s *= 18446744073709551616.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= 18446744073709551616.f;
+    }
+    const float inv = s == 0.f ? 0.f : __builtin_amdgcn_rcpf(s);
     uint32_t code[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) code[j] = zero ? OFF : quantise<BITS>(rows[u].get(j) * up, s, inv);
+    for (int j = 0; j < 8; ++j) code[j] = quantise<BITS>(x[j], s, inv);
     char* codes = kv_codes<HD, BITS>(a, p);
     if constexpr (BITS == 8) {
       u32x2 w;
@@ -212,7 +232,7 @@ __global__ __launch_bounds__(256) void k_kv_read(KvRows a) {
   uint16_t sb[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    place[u] = kv_place<HD>(a, (static_cast<uint64_t>(blockIdx.x) * U + u) * 256 + threadIdx.x);
+    place[u] = kv_place<HD, U>(a, u);
     w[u] = u32x2{0, 0};
     sb[u] = 0;
     if (place[u].live) {
@@ -254,13 +274,21 @@ void by_cache(int dtype, const gm_kv_cache& c, F f) {
   else head(f16_t());
 }
 
-// f(items per thread, grid): one where there are few, so that they spread over the GPU.
+// f(items per thread, rows, grid): four items a thread where a head's rows fill such a
+// workgroup, one where they do not.
 template <typename F>
-void kv_launch(const KvRows& a, F f) {
-  const uint64_t items = static_cast<uint64_t>(a.B) * a.n * a.c.heads * 2 * (a.c.head_dim / 8);
-  auto blocks = [&](int u) { return dim3(static_cast<uint32_t>((items + 256 * u - 1) / (256 * u))); };
-  if (items >= 256 * 4 * 2048) f(std::integral_constant<int, 4>(), blocks(4));
-  else f(std::integral_constant<int, 1>(), blocks(1));
+void kv_launch(KvRows a, F f) {
+  const uint64_t heads = static_cast<uint64_t>(a.B) * a.c.heads * 2;
+  const uint64_t items = static_cast<uint64_t>(a.n) * (a.c.head_dim / 8);   // of a head
+  a.by_n = Div(a.n);
+  a.by_heads = Div(a.c.heads);
+  if (items >= 1024) {
+    const uint64_t blocks = (items + 1023) / 1024;
+    a.by_blocks = Div(static_cast<uint32_t>(blocks));
+    f(std::integral_constant<int, 4>(), a, dim3(static_cast<uint32_t>(heads * blocks)));
+  } else {
+    f(std::integral_constant<int, 1>(), a, dim3(static_cast<uint32_t>((heads * items + 255) / 256)));
+  }
 }
 
 }  // namespace
@@ -268,8 +296,7 @@ void kv_launch(const KvRows& a, F f) {
 void launch_kv_write(const gm_kv_cache& c, int dtype, int B, int n, const gm_tensor& k,
                      const gm_tensor& v, const int32_t* start, const int32_t* count,
                      const int32_t* mask, hipStream_t s) {
-  const KvRows a{c, k, v, start, count, mask, B, n, Div(n), Div(c.heads)};
-  kv_launch(a, [&](auto u, dim3 grid) {
+  kv_launch(KvRows{c, k, v, start, count, mask, B, n}, [&](auto u, const KvRows& a, dim3 grid) {
     by_cache(dtype, c, [&](auto t, auto hd, auto bits) {
       hipLaunchKernelGGL((k_kv_write<decltype(t), decltype(hd)::value, decltype(bits)::value, decltype(u)::value>),
                          grid, dim3(256), 0, s, a);
@@ -279,8 +306,7 @@ void launch_kv_write(const gm_kv_cache& c, int dtype, int B, int n, const gm_ten
 
 void launch_kv_read(const gm_kv_cache& c, int dtype, int B, int n, const int32_t* start,
                     const int32_t* count, const gm_tensor& k, const gm_tensor& v, hipStream_t s) {
-  const KvRows a{c, k, v, start, count, nullptr, B, n, Div(n), Div(c.heads)};
-  kv_launch(a, [&](auto u, dim3 grid) {
+  kv_launch(KvRows{c, k, v, start, count, nullptr, B, n}, [&](auto u, const KvRows& a, dim3 grid) {
     by_cache(dtype, c, [&](auto t, auto hd, auto bits) {
       hipLaunchKernelGGL((k_kv_read<decltype(t), decltype(hd)::value, decltype(bits)::value, decltype(u)::value>),
                          grid, dim3(256), 0, s, a);
