@@ -332,15 +332,20 @@ struct CachedPlan {
 };
 
 // The MFMA kernel takes 16-bit dtypes: 16 columns of a product are shared by query
-// rows and 32-channel groups.  In fp32 a workgroup takes one row.
+// rows and 32-channel groups.  In fp32 a workgroup takes one row.  Chunks: as many as
+// bring 512 workgroups, two a CU, of 128 keys at the least (us a call at 256 / 512 /
+// 768 / 1024 workgroups: one sequence of 32000 keys, 32 heads of 128, 4 bits, 46.1 /
+// 38.0 / 38.2 / 41.8; 32 of 8190 with 8 heads 85.8 / 68.9 / 73.4 / 73.8; 8 of 2000 with
+// 8 heads, 8 bits, 16.6 / 15.9 / 20.0 / 20.0; at 128 / 256 / 512 keys: one of 4000 keys
+// with 8 heads 11.8 / 12.0 / 14.4, 8 of 640 with 12 heads of 64 9.7 / 10.7 / 10.7).
 CachedPlan cached_plan(const gm_kv_cache& c, int dtype, int B, int Sq, int n_heads) {
   CachedPlan p;
   p.rows = Sq * (n_heads / c.heads);
   const int per_block = dtype == kF32 ? 1 : 16 / (c.head_dim / kKvGroup);
   p.blocks = (p.rows + per_block - 1) / per_block;
   const long long wgs = static_cast<long long>(B) * c.heads * p.blocks;
-  long long want = (1024 + wgs - 1) / wgs;
-  const long long most = (c.max_seq + 255) / 256;
+  long long want = (512 + wgs - 1) / wgs;
+  const long long most = (c.max_seq + 127) / 128;
   want = want < most ? want : most;
   p.nsplit = static_cast<int>(want < 64 ? want : 64);
   return p;
@@ -497,9 +502,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <int NG>
 __device__ __forceinline__ float group_sum(float v) {
   if constexpr (NG >= 2)
-    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0xB1, 0xf, 0xf, true));
+    v += dpp_or_zero<0xB1, 0xf>(v);   // lanes 1 0 3 2
   if constexpr (NG == 4)
-    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x4E, 0xf, 0xf, true));
+    v += dpp_or_zero<0x4E, 0xf>(v);   // lanes 2 3 0 1
   return v;
 }
 
@@ -540,10 +545,22 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 //    scores a lane holds are the 8 k slots of its B operand, so w needs no exchange; A row m
 //    of product i is channel (HD / 16) m + i, a lane reading HD / 16 channels of 8 keys.
 //    A lane's own column counts where the channel's group is the column's.
+// Heads with more rows than a set of columns holds (4 of 128 channels) take more
+// workgroups, which read the same codes again, mostly from cache; two sets in one
+// workgroup need 256 registers and gain nothing (16 sequences of 4000 keys, 32/4 heads,
+// 4 bits: 23.0 us a set each, 23.6 two; 8 bits 31.3 and 43.0).
+// The tile being worked on and its successor, which arrives meanwhile, are both in
+// registers.  512 workgroups of 4 wavefronts: 32 sequences of 8190 keys, 32/8 heads of
+// 128, 4 bits, 68.9 us (4.4 TB/s; a large copy reaches 4.8); 4 of 8000 keys, 32 heads, 8
+// bits, 59 us (4.7 TB/s).
 // The query is divided by a power of two as well (largest element to 2^14), so that bf16
 // and fp16 rows become fp16 without loss.  The maximum m moves lazily (by more than 2^8).
+// Wavefronts per SIMD that the registers of a tile, its successor and O leave room for.
+constexpr int cached_waves(int hd, int bits) { return hd == 128 ? (bits == 4 ? 3 : 2) : hd == 64 ? 3 : 4; }
+
 template <typename T, int HD, int BITS, bool CAP>
-__global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_kv_cache c,
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(cached_waves(HD, BITS), cached_waves(HD, BITS))))
+void k_cached_mfma(gm_cached_attention a, gm_kv_cache c,
                                                      CachedPlan plan) {
   constexpr int OFF = 1 << (BITS - 1), NWV = 4, KB = 32;
   constexpr int NG = HD / kKvGroup, RB = 16 / NG;   // groups, rows per block
@@ -558,13 +575,14 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
   const int r = w.blk * RB + n / NG;                // this column's query row
   const bool row_ok = r < plan.rows;
   const int GQ = a.n_heads / c.heads, rr = row_ok ? r : 0, i = rr / GQ, h = w.kvh * GQ + rr % GQ;
-  const int qpos = row_ok ? w.len - a.Sq + i : -1;
+  // (columns past the last row repeat row 0 and are not used)
+  const int qpos = w.len - a.Sq + i, open = w.len - a.Sq;   // every row sees keys up to `open`
   const float slope2 = a.scores.slopes ? a.scores.slopes[h] * kLog2e : 0.f;
 
   // ---- the query as B operands: k step st, slots 2 d and 2 d + 1 hold the channels whose
   // codes the unpacking below puts there
   f16x8 qf[NG];
-  float c0, up;                                     // start of the sums of S; half of their unit
+  float c0, up;                                     // start of the sums of S; part of their unit
   float c2 = CAP ? a.scores.scale * (2.f * kLog2e) / a.scores.softcap : a.scores.scale * kLog2e;
   {
     constexpr int NC = HD / 4;
@@ -598,9 +616,11 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
     sum += __shfl_xor(sum, 16, 64);
     sum += __shfl_xor(sum, 32, 64);
     c0 = -static_cast<float>(OFF) * kTiny * sum;
-    // the sums' unit 2^24 / 2^(14 - ex) in two factors, each far from the ends of fp32
-    up = ldexpf(1.f, (10 + ex) / 2);
-    c2 = ldexpf(c2, 10 + ex - (10 + ex) / 2);
+    // the sums' unit 2^24 / 2^(14 - ex); of rows near the ends of fp32 a part goes
+    // to the K scales
+    const int part = 10 + ex > 90 ? 10 + ex - 90 : 10 + ex < -90 ? 100 + ex : 0;
+    up = ldexpf(1.f, part);
+    c2 = ldexpf(c2, 10 + ex - part);
   }
   const float capc = a.scores.softcap * kLog2e;
 
@@ -617,7 +637,7 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
     uint32_t k[2][KD], v[8][VD];
     u32x4 ks, vs;
     u32x2 valid;
-  } cur;
+  };
   auto fetch = [&](int kb, Tile& x) {
     const long long row = static_cast<long long>(kb) * (HD * BITS / 8);
 #pragma unroll
@@ -641,11 +661,8 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
     off[1][j] = static_cast<_Float16>(OFF * kTiny * (BITS == 4 ? 16.f : 1.f));
   }
 
-  int kb = w.k0 + KB * wave;
-  if (kb < w.k1) fetch(kb, cur);
-  for (; kb < w.k1; kb += NWV * KB) {
-    Tile x = cur;
-    if (kb + NWV * KB < w.k1) fetch(kb + NWV * KB, cur);
+  const bool wide = __ballot(up != 1.f) != 0;
+  auto step = [&](int kb, const Tile& x) {
     // ---- scores of 8 keys
     float s[8];
 #pragma unroll
@@ -670,18 +687,36 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[4 * u + e] = acc[e];
     }
-    float top = -INFINITY;
+    float sk[8], sv[8], most = 0.f, top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      sk[j] = __uint_as_float(j % 2 ? x.ks[j / 2] & 0xffff0000u : x.ks[j / 2] << 16);
+      sv[j] = __uint_as_float(j % 2 ? x.vs[j / 2] & 0xffff0000u : x.vs[j / 2] << 16);
+    }
+    if (wide) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sk[j] *= up;
+    }
     const float dist = static_cast<float>(qpos - kb - 8 * g);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float sk = bf16_value(j % 2 ? x.ks[j / 2] >> 16 : x.ks[j / 2] & 0xffffu);
-      float y = group_sum<NG>(s[j] * (sk * up)) * c2;
+      float y = group_sum<NG>(s[j] * sk[j]) * c2;
       if constexpr (CAP) y = fmaf(-2.f * capc, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f), capc);
-      y = fmaf(-slope2, dist - static_cast<float>(j), y);
-      bool ok = kb + 8 * g + j <= qpos && kb + 8 * g + j < w.k1;
-      if (valid) ok = ok && ((x.valid[j / 4] >> (8 * (j % 4))) & 255u) != 0;
-      s[j] = ok ? y : -INFINITY;
+      s[j] = fmaf(-slope2, dist - static_cast<float>(j), y);
+    }
+    if (valid || kb + KB - 1 > open || kb + KB > w.k1) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        bool ok = kb + 8 * g + j <= qpos && kb + 8 * g + j < w.k1;
+        if (valid) ok = ok && ((x.valid[j / 4] >> (8 * (j % 4))) & 255u) != 0;
+        s[j] = ok ? s[j] : -INFINITY;
+        sv[j] = ok ? sv[j] : 0.f;                   // (it may be NaN)
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
       top = fmaxf(top, s[j]);
+      most = fmaxf(most, sv[j]);
     }
     if (__ballot(top > m + kTau)) {
       top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -692,14 +727,6 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
 #pragma unroll
       for (int e = 0; e < NI; ++e) o[e] *= f;
       m = mn;
-    }
-    // ---- V scales; hidden keys' are 0 (they may be NaN)
-    float sv[8], most = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sv[j] = bf16_value(j % 2 ? x.vs[j / 2] >> 16 : x.vs[j / 2] & 0xffffu);
-      sv[j] = s[j] == -INFINITY ? 0.f : sv[j];
-      most = fmaxf(most, sv[j]);
     }
     if (__ballot(most > 8.f * bound)) {
       most = fmaxf(most, __shfl_xor(most, 16, 64));
@@ -754,6 +781,19 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
         o[e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, f) - off[0], wf, o[e], 0, 0, 0);
       }
     }
+  };
+  // ---- two tiles in turn, one being worked on while the other arrives
+  Tile x0, x1;
+  int kb = w.k0 + KB * wave;
+  if (kb < w.k1) fetch(kb, x0);
+  while (kb < w.k1) {
+    if (kb + NWV * KB < w.k1) fetch(kb + NWV * KB, x1);
+    step(kb, x0);
+    kb += NWV * KB;
+    if (kb >= w.k1) break;
+    if (kb + NWV * KB < w.k1) fetch(kb + NWV * KB, x0);
+    step(kb, x1);
+    kb += NWV * KB;
   }
   // ---- the wavefront's normalised output: rows 4 g + e of product x are channels
   // NI (4 g + e) + x, of group g NG / 4
@@ -802,25 +842,58 @@ __global__ __launch_bounds__(256) void k_cached_mfma(gm_cached_attention a, gm_k
   }
 }
 
-// The chunks of a row merged in their order.
+// The chunks of a row merged, a workgroup per row: the weights by the first wavefront,
+// a lane per chunk (at most 64), then the chunks in 256 / HD parts, each in order, and
+// the parts in theirs.
 template <typename T, int HD>
-__global__ __launch_bounds__(HD) void k_cached_merge(gm_cached_attention a, gm_kv_cache c,
-                                                     CachedPlan plan) {
-  const int ch = threadIdx.x;
+__global__ __launch_bounds__(256) void k_cached_merge(gm_cached_attention a, gm_kv_cache c,
+                                                      CachedPlan plan) {
+  constexpr int PARTS = 256 / HD;
+  __shared__ float s_w[64], s_o[PARTS][HD];
+  const int tid = threadIdx.x, ch = tid % HD, of = tid / HD;
   int x = blockIdx.x;
   const int r = x % plan.rows;
   x /= plan.rows;
   const int kvh = x % c.heads, b = x / c.heads;
   const float* part = cached_part<HD>(a, c, plan, b, kvh, r, 0);
-  float M = -INFINITY, L = 0.f, O = 0.f;
-  for (int s = 0; s < plan.nsplit; ++s) M = fmaxf(M, part[s * (HD + 2)]);
-  for (int s = 0; s < plan.nsplit; ++s) {
-    const float ms = part[s * (HD + 2)], ls = part[s * (HD + 2) + 1];
-    const float f = ls == 0.f ? 0.f : ls * __builtin_amdgcn_exp2f(ms - M);
-    L += f;
-    O += f == 0.f ? 0.f : f * part[s * (HD + 2) + 2 + ch];
+  constexpr int U = 8;
+  float o[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int s = of + u * PARTS;
+    o[u] = s < plan.nsplit ? part[s * (HD + 2) + 2 + ch] : 0.f;
   }
-  cached_out<T>(a, c, b, kvh, r)[ch] = from_f32<T>(L == 0.f ? 0.f : O / L);
+  if (tid < 64) {
+    const bool on = tid < plan.nsplit;
+    const float m = on ? part[tid * (HD + 2)] : -INFINITY, l = on ? part[tid * (HD + 2) + 1] : 0.f;
+    const float M = wave_max(m);
+    const float w = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - M);
+    const float W = wave_sum(w);
+    s_w[tid] = w == 0.f ? 0.f : w / W;
+  }
+  __syncthreads();
+  float sum = 0.f;
+  for (int s0 = 0; s0 < plan.nsplit; s0 += U * PARTS) {
+    if (s0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int s = s0 + of + u * PARTS;
+        o[u] = s < plan.nsplit ? part[s * (HD + 2) + 2 + ch] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + of + u * PARTS;
+      const float w = s < plan.nsplit ? s_w[s] : 0.f;
+      sum += w == 0.f ? 0.f : w * o[u];
+    }
+  }
+  s_o[of][ch] = sum;
+  __syncthreads();
+  if (of) return;
+#pragma unroll
+  for (int p = 1; p < PARTS; ++p) sum += s_o[p][ch];
+  cached_out<T>(a, c, b, kvh, r)[ch] = from_f32<T>(sum);
 }
 
 }  // namespace
@@ -846,7 +919,7 @@ void launch_attention_cached(const gm_cached_attention& a, hipStream_t s) {
     else
       hipLaunchKernelGGL((k_cached_mfma<T, HD, BITS, false>), grid, block, 0, s, a, c, p);
     if (p.nsplit > 1)
-      hipLaunchKernelGGL((k_cached_merge<T, HD>), dim3(heads * p.rows), dim3(HD), 0, s, a, c, p);
+      hipLaunchKernelGGL((k_cached_merge<T, HD>), dim3(heads * p.rows), block, 0, s, a, c, p);
   });
 }
 
