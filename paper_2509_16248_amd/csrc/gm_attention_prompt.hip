@@ -39,6 +39,7 @@ __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, 
   auto score = [&](int j) {
     const T* k = kb + j * a.k.token;
     float s = 0.f;
+#pragma unroll 4
     for (int c = 0; c < HD; ++c) s = fmaf(to_f32(q[c]), to_f32(k[c]), s);
     return modify_score(s * a.scores.scale, a.scores.softcap, slope, fabsf(static_cast<float>(qpos - j)));
   };
@@ -72,27 +73,166 @@ __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, 
     if (lane + 64 * c < HD) out[lane + 64 * c] = from_f32<T>(l == 0.f ? 0.f : o[c] / l);
 }
 
-// A wavefront per (query, head).
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_prompt_rows(gm_prompt_attention a) {
-  const uint64_t e = blockIdx.x * 4ull + (threadIdx.x >> 6);
-  const int i = static_cast<int>(e % a.Sq);
-  const uint64_t r = e / a.Sq;
-  const int h = static_cast<int>(r % a.n_heads);
-  if (r / a.n_heads >= static_cast<uint64_t>(a.B)) return;
-  prompt_row<T, HD>(a, static_cast<int>(r / a.n_heads), h, i);
+// ------------------------------------------------------------ fp32
+// Workgroup = 32 queries of one (sequence, head), as k_attn_f32 (gm_attention.hip)
+// splits and multiplies: its 4 wavefronts take the tiles of 32 keys in turn, each with
+// an online softmax of its own, and are merged in LDS; S^T = K Q^T and O^T += V^T P^T on
+// v_mfma_f32_32x32x2_f32 with operands straight from global memory, a lane holding 16
+// scores of one query.  What each lane's query may see of a tile is settled first, and
+// a tile that shows no query anything is not loaded.  Queries whose sums came out not
+// finite are computed again by prompt_row: a hidden key's weight is 0, but its product
+// with an Inf or NaN value is not.
+template <int HD, bool CAP>
+__global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
+  constexpr int NC = HD / 8, CB = HD / 32, NW = 4;
+  typedef float f32x4a __attribute__((ext_vector_type(4)));
+  __shared__ float s_m[NW][32], s_l[NW][32];
+  __shared__ float s_o[NW][HD][33];
+  __shared__ uint32_t s_odd[NW];
+  const int nqb = (a.Sq + 31) / 32;
+  int x = blockIdx.x;
+  const int qb = a.causal ? nqb - 1 - x % nqb : x % nqb;
+  x /= nqb;
+  const int h = x % a.n_heads, b = x / a.n_heads, kvh = h / (a.n_heads / a.kv_heads);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l32 = lane & 31, g = lane >> 5;
+  const int Sq = a.Sq, Sk = a.Sk, q0 = qb * 32, qi = q0 + l32, qpos = qi + a.q_offset;
+  const int qc = qi < Sq ? qi : Sq - 1;
+  const float* q = static_cast<const float*>(a.q.p) + b * a.q.batch + qc * a.q.token + h * a.q.head + 4 * g;
+  const float* kb = static_cast<const float*>(a.k.p) + b * a.k.batch + kvh * a.k.head;
+  const float* vb = static_cast<const float*>(a.v.p) + b * a.v.batch + kvh * a.v.head;
+  const int32_t* mk = a.key_mask ? a.key_mask + static_cast<long long>(b) * Sk : nullptr;
+  const int32_t* kd = a.q_doc ? a.k_doc + static_cast<long long>(b) * Sk : nullptr;
+  const int qd = a.q_doc ? a.q_doc[static_cast<long long>(b) * Sq + qc] : 0;
+  const float slope = a.scores.slopes ? a.scores.slopes[h] : 0.f;
+  const int pre = a.causal && a.prefix ? a.prefix[b] : 0;
+  int kend = Sk;                               // keys this lane's query may see end here
+  if (a.causal) {
+    kend = qpos + 1 > pre ? qpos + 1 : pre;
+    kend = kend < Sk ? kend : Sk;
+  }
+  int ktop = Sk;                               // and those of the workgroup's queries here
+  if (a.causal) {
+    ktop = q0 + 32 + a.q_offset > pre ? q0 + 32 + a.q_offset : pre;
+    ktop = ktop < Sk ? ktop : Sk;
+  }
+  f32x4a qf[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const f32x4a*>(q + 8 * c);
+  f32x16 o[CB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
+  float m = -INFINITY, l = 0.f;
+  for (int k0 = 32 * wave; k0 < ktop; k0 += 32 * NW) {
+    uint32_t vis = 0;                          // bit e: score e's key is visible
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int key = k0 + 8 * (e / 4) + 4 * g + e % 4;
+      bool ok = key < kend;
+      const int kc = key < Sk ? key : Sk - 1;
+      if (mk) ok = ok && mk[kc] != 0;
+      if (kd) ok = ok && kd[kc] == qd;
+      vis |= (ok ? 1u : 0u) << e;
+    }
+    if (__ballot(vis != 0) == 0) continue;
+    const int kr = k0 + l32 < Sk ? k0 + l32 : Sk - 1;
+    const float* k = kb + kr * a.k.token + 4 * g;
+    f32x4a kf[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const f32x4a*>(k + 8 * c);
+    float vf[16][CB];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      const int key = k0 + 8 * (t / 4) + 4 * g + t % 4;
+      const float* v = vb + (key < Sk ? key : Sk - 1) * a.v.token + l32;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) vf[t][c] = v[32 * c];
+    }
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][r], qf[c][r], s, 0, 0, 0);
+    float top = m;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int key = k0 + 8 * (e / 4) + 4 * g + e % 4;
+      const float y = modify_score(s[e] * a.scores.scale, CAP ? a.scores.softcap : 0.f, slope,
+                                   fabsf(static_cast<float>(qpos - key)));
+      s[e] = vis >> e & 1 ? y : -INFINITY;
+      top = fmaxf(top, s[e]);
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float corr = top == -INFINITY ? 1.f : expf(m - top);   // (m = -inf: 0)
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = s[e] == -INFINITY ? 0.f : expf(s[e] - top);
+      sum += s[e];
+    }
+    l = l * corr + sum;
+    m = top;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[c][e] *= corr;
+#pragma unroll
+      for (int t = 0; t < 16; ++t) o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[t][c], s[t], o[c], 0, 0, 0);
+    }
+  }
+  l += __shfl_xor(l, 32, 64);
+  float odd = 0.f * l;
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) odd = fmaf(o[c][e], 0.f, odd);
+  const unsigned long long odd_lanes = __ballot(odd != 0.f);   // (NaN != 0)
+  if (lane == 0) s_odd[wave] = static_cast<uint32_t>(odd_lanes) | static_cast<uint32_t>(odd_lanes >> 32);
+  if (g == 0) {
+    s_m[wave][l32] = m;
+    s_l[wave][l32] = l;
+  }
+#pragma unroll
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s_o[wave][32 * c + 8 * (e / 4) + 4 * g + e % 4][l32] = o[c][e];
+  __syncthreads();
+  const uint32_t again = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
+  for (int e = threadIdx.x; e < 32 * HD; e += 256) {
+    const int c = e % HD, i = e / HD;
+    if (q0 + i >= Sq) break;
+    if (again >> i & 1) continue;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w][i]);
+    float L = 0.f, O = 0.f;
+    if (M != -INFINITY)
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float f = s_m[w][i] == -INFINITY ? 0.f : expf(s_m[w][i] - M);
+        L += s_l[w][i] * f;
+        O += s_o[w][c][i] * f;
+      }
+    static_cast<float*>(a.out.p)[b * a.out.batch + (q0 + i) * a.out.token + h * a.out.head + c] =
+        L > 0.f ? O / L : 0.f;
+  }
+  if (__builtin_expect(again != 0, 0))
+    for (int i = wave; i < 32; i += NW)
+      if ((again >> i & 1) && q0 + i < Sq) prompt_row<float, HD>(a, b, h, q0 + i);
 }
 
-template <typename T>
-void prompt_rows(const gm_prompt_attention& a, hipStream_t s) {
-  const uint64_t rows = static_cast<uint64_t>(a.B) * a.Sq * a.n_heads;
-  const dim3 grid(static_cast<unsigned>((rows + 3) / 4)), block(256);
-  if (a.head_dim == 32) hipLaunchKernelGGL((k_prompt_rows<T, 32>), grid, block, 0, s, a);
-  else if (a.head_dim == 64) hipLaunchKernelGGL((k_prompt_rows<T, 64>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_prompt_rows<T, 128>), grid, block, 0, s, a);
+template <int HD>
+void prompt_f32(const gm_prompt_attention& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.Sq + 31) / 32) * a.n_heads * a.B), block(256);
+  if (a.scores.softcap > 0.f) hipLaunchKernelGGL((k_prompt_f32<HD, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_prompt_f32<HD, false>), grid, block, 0, s, a);
 }
 
-// ------------------------------------------------------------ 16-bit, head size 64 and 128
+// ------------------------------------------------------------ 16-bit
 // 32 bits of four consecutive int32, at any 4-byte address.
 typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -504,10 +644,15 @@ void prompt_flash(const gm_prompt_attention& a, hipStream_t s) {
 }  // namespace
 
 void launch_attention_prompt(const gm_prompt_attention& a, hipStream_t s) {
-  if (a.dtype == kF32) prompt_rows<float>(a, s);
-  else if (a.head_dim == 32) a.dtype == kBF16 ? prompt_rows<bf16_t>(a, s) : prompt_rows<f16_t>(a, s);
-  else if (a.dtype == kBF16) a.head_dim == 64 ? prompt_flash<bf16_t, 64>(a, s) : prompt_flash<bf16_t, 128>(a, s);
-  else a.head_dim == 64 ? prompt_flash<f16_t, 64>(a, s) : prompt_flash<f16_t, 128>(a, s);
+  auto head = [&](auto hd) {
+    constexpr int HD = decltype(hd)::value;
+    if (a.dtype == kF32) prompt_f32<HD>(a, s);
+    else if (a.dtype == kBF16) prompt_flash<bf16_t, HD>(a, s);
+    else prompt_flash<f16_t, HD>(a, s);
+  };
+  if (a.head_dim == 32) head(std::integral_constant<int, 32>());
+  else if (a.head_dim == 64) head(std::integral_constant<int, 64>());
+  else head(std::integral_constant<int, 128>());
 }
 
 }  // namespace gm

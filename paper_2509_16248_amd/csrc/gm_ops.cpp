@@ -178,9 +178,9 @@ int gm_attention(const gm_prompt_attention* a, hipStream_t stream) {
       misaligned(a->prefix, 4))
     return inval("int32 arrays must be 4-byte aligned");
   if (a->B == 0 || a->Sq == 0) return GM_OK;
-  // a launch has fewer than 2^32 threads, a wavefront per row at the most
-  if (static_cast<double>(a->B) * a->Sq * a->n_heads >= 67108860.0)
-    return inval("B * Sq * n_heads must be below 2^26 - 4");
+  // a launch has fewer than 2^32 threads, 256 for 32 query rows of a head
+  if (static_cast<double>(a->B) * a->n_heads * ((a->Sq + 31) / 32) >= 16777216.0)
+    return inval("B * n_heads * ceil(Sq / 32) must be below 2^24");
   launch_attention_prompt(*a, stream);
   return launched();
 }
