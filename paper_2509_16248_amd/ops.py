@@ -74,22 +74,32 @@ def _first(t: torch.Tensor, name: str):
     return t.dtype, code, t.device
 
 
+# The current stream's handle by device index: torch.cuda.current_stream without the
+# Stream object around it, which takes as long to make as half a launch.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _on(device, stream, call, tensors):
     """call(stream handle) with the device current; on a stream given by the
     caller, what the call allocates belongs to that stream, and the allocator
-    is told that the tensors are in use there."""
-    if stream is None and device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream(device).cuda_stream)
+    is told that tensors() are in use there."""
     if stream is None:
+        if device.index == torch.cuda.current_device():
+            return call(_raw_stream(device.index))
         with torch.cuda.device(device):
-            return call(torch.cuda.current_stream(device).cuda_stream)
+            return call(_raw_stream(device.index))
     if stream.device != device:
         raise ValueError(f"the stream must be on {device}, not {stream.device}")
     with torch.cuda.stream(stream):
-        for t in tensors:
+        for t in tensors():
             if t is not None:
                 t.record_stream(stream)
         return call(stream.cuda_stream)
+
+
+def _tensor(*fields) -> gm.gm_tensor:
+    return gm.gm_tensor.from_buffer_copy(_TENSOR.pack(*fields))
 
 
 class KvCache:
@@ -125,6 +135,7 @@ class KvCache:
                                 self.v.data_ptr(), self.k_scale.data_ptr(),
                                 self.v_scale.data_ptr(),
                                 self.valid.data_ptr() if masked else None)
+        self._workspace = {}      # bytes that attention needs, by dtype and shape of the queries
 
     def nbytes(self) -> int:
         return sum(t.numel() * t.element_size() for t in self._tensors())
@@ -149,13 +160,13 @@ class KvCache:
         if B > self.batch:
             raise ValueError(f"the rows' batch {B} exceeds the cache's {self.batch}")
         shape = (B, n, self.heads, self.head_dim)
-        kt, vt = (gm.gm_tensor.from_buffer_copy(_TENSOR.pack(*_rows(t, name, shape, dtype, device)))
-                  for t, name in ((k, "k"), (v, "v")))
+        kt = _tensor(*_rows(k, "k", shape, dtype, device))
+        vt = _tensor(*_rows(v, "v", shape, dtype, device))
         st, ct = _ints(start, "start", (B,), device), _ints(count, "count", (B,), device)
         mt = _ints(mask, "mask", (B, n), device)
         _on(device, stream,
             lambda s: gm.gm_kv_write(self.c, code, B, n, kt, vt, st, ct, mt, s),
-            (k, v, start, count, mask, *self._tensors()))
+            lambda: (k, v, start, count, mask, *self._tensors()))
 
     def read(self, n: int, start: Optional[torch.Tensor] = None,
              count: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
@@ -180,13 +191,12 @@ class KvCache:
             k, v = out if out is not None else (
                 torch.empty(shape, dtype=dtype, device=device),
                 torch.empty(shape, dtype=dtype, device=device))
-            kt, vt = (gm.gm_tensor.from_buffer_copy(
-                _TENSOR.pack(*_rows(t, name, shape, dtype, device)))
-                for t, name in ((k, "k"), (v, "v")))
+            kt = _tensor(*_rows(k, "k", shape, dtype, device))
+            vt = _tensor(*_rows(v, "v", shape, dtype, device))
             gm.gm_kv_read(self.c, code, B, n, st, ct, kt, vt, s)
             return k, v
 
-        return _on(device, stream, call, (start, count, *(out or ()), *self._tensors()))
+        return _on(device, stream, call, lambda: (start, count, *(out or ()), *self._tensors()))
 
 
 def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
@@ -212,7 +222,10 @@ def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
         raise ValueError("lengths is missing")
     qt, lt = _rows(q, "q", shape, dtype, device), _ints(lengths, "lengths", (B,), device)
     sl = _ints(slopes, "slopes", (H,), device, torch.float32)
-    need = gm.gm_attention_cached_workspace(cache.c, code, B, Sq, H)
+    need = cache._workspace.get((code, B, Sq, H))
+    if need is None:
+        need = gm.gm_attention_cached_workspace(cache.c, code, B, Sq, H)
+        cache._workspace[code, B, Sq, H] = need
 
     def call(s):
         res = torch.empty(shape, dtype=dtype, device=device) if out is None else out
@@ -225,7 +238,7 @@ def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
         gm.gm_attention_cached(a, s)
         return res
 
-    return _on(device, stream, call, (q, out, lengths, slopes, *cache._tensors()))
+    return _on(device, stream, call, lambda: (q, out, lengths, slopes, *cache._tensors()))
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False,
@@ -264,4 +277,5 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool
         gm.gm_attention(a, s)
         return res
 
-    return _on(device, stream, call, (q, k, v, out, slopes, key_mask, q_doc, k_doc, prefix))
+    return _on(device, stream, call,
+               lambda: (q, k, v, out, slopes, key_mask, q_doc, k_doc, prefix))
