@@ -337,15 +337,23 @@ struct CachedPlan {
 // 768 / 1024 workgroups: one sequence of 32000 keys, 32 heads of 128, 4 bits, 46.1 /
 // 38.0 / 38.2 / 41.8; 32 of 8190 with 8 heads 85.8 / 68.9 / 73.4 / 73.8; 8 of 2000 with
 // 8 heads, 8 bits, 16.6 / 15.9 / 20.0 / 20.0; at 128 / 256 / 512 keys: one of 4000 keys
-// with 8 heads 11.8 / 12.0 / 14.4, 8 of 640 with 12 heads of 64 9.7 / 10.7 / 10.7).
+// with 8 heads 11.8 / 12.0 / 14.4).  Up to 65536 / head_dim positions one chunk, which
+// saves the merge's launch (one chunk / split: 8 sequences, 12 heads of 64, 8 bits,
+// capacity 1024, length 300 6.7 / 8.3, 640 8.1 / 9.1, 1000 10.5 / 10.4; capacity 2048, 2000
+// 16.1 / 11.0; one, 32 heads of 128, 4 bits, capacity 256 6.4 / 7.9, 512 8.0 / 7.9, 1024
+// 12.0 / 8.6): a call knows the capacity, a cache in use is half full on average.  The
+// fp32 kernel, one row a workgroup, wants 1024 of them (8 sequences of 2000 keys, 32/8
+// heads of 128, at 256 / 512 / 1024 / 2048: 60.6 / 43.2 / 37.6 / 38.7) and half the positions
+// (one, 12 heads of 64, capacity 1024, length 300 7.6 / 7.3, 1000 15.7 / 7.5).
 CachedPlan cached_plan(const gm_kv_cache& c, int dtype, int B, int Sq, int n_heads) {
   CachedPlan p;
   p.rows = Sq * (n_heads / c.heads);
   const int per_block = dtype == kF32 ? 1 : 16 / (c.head_dim / kKvGroup);
   p.blocks = (p.rows + per_block - 1) / per_block;
   const long long wgs = static_cast<long long>(B) * c.heads * p.blocks;
-  long long want = (512 + wgs - 1) / wgs;
-  const long long most = (c.max_seq + 127) / 128;
+  const int target = dtype == kF32 ? 1024 : 512, room = dtype == kF32 ? 32768 : 65536;
+  long long want = (target + wgs - 1) / wgs;
+  const long long most = static_cast<long long>(c.max_seq) * c.head_dim > room ? (c.max_seq + 127) / 128 : 1;
   want = want < most ? want : most;
   p.nsplit = static_cast<int>(want < 64 ? want : 64);
   return p;
@@ -416,41 +424,57 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
   const uint16_t* ks = static_cast<const uint16_t*>(c.k_scale) + sbase;
   const uint16_t* vs = static_cast<const uint16_t*>(c.v_scale) + sbase;
   const uint8_t* valid = c.valid ? c.valid + static_cast<long long>(w.b) * c.max_seq : nullptr;
-  auto codes = [&](const char* p, float (&x)[8]) {
-    if constexpr (BITS == 8) {
-      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+  constexpr int W = BITS / 4;                  // words of 8 codes
+  auto codes = [&](const uint32_t (&v)[W], float (&x)[8]) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        x[j] = static_cast<float>(static_cast<int>((v[j / 4] >> (8 * (j % 4))) & 255u) - OFF);
-    } else {
-      const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        x[j] = static_cast<float>(static_cast<int>((v >> (4 * j)) & 15u) - OFF);
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t code = BITS == 8 ? (v[j / 4 % W] >> (8 * (j % 4))) & 255u : (v[0] >> (4 * j)) & 15u;
+      x[j] = static_cast<float>(static_cast<int>(code) - OFF);
     }
   };
   float m = -INFINITY, l = 0.f, o[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) o[j] = 0.f;
-  for (int key = w.k0 + wave * KPW + grp; key < k1; key += NG) {
-    float kx[8], vx[8];
-    codes(kc + static_cast<long long>(key) * (HD * BITS / 8), kx);
-    codes(vc + static_cast<long long>(key) * (HD * BITS / 8), vx);
-    const float sk = bf16_value(ks[key]), sv = bf16_value(vs[key]);
-    float s = 0.f;
+  // U keys a lane group, their rows loaded together (keys past the end read the
+  // chunk's first)
+  constexpr int U = 4;
+  for (int key0 = w.k0 + wave * KPW + grp; key0 < k1; key0 += U * NG) {
+    uint32_t kr[U][W], vr[U][W];
+    uint16_t kscale[U], vscale[U];
+    uint8_t on[U];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(q[j], kx[j], s);
-    s *= sk;
+    for (int u = 0; u < U; ++u) {
+      const int key = key0 + u * NG < k1 ? key0 + u * NG : w.k0;
+      const long long row = static_cast<long long>(key) * (HD * BITS / 8);
 #pragma unroll
-    for (int off = G / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
-    if (valid && !valid[key]) continue;   // the same for the whole lane group
-    s = modify_score(s * a.scores.scale, a.scores.softcap, slope, static_cast<float>(qpos - key));
-    const float mn = fmaxf(m, s);
-    const float corr = m == mn ? 1.f : expf(m - mn), p = s == -INFINITY ? 0.f : expf(s - mn);
-    l = l * corr + p;
+      for (int j = 0; j < W; ++j) {
+        kr[u][j] = reinterpret_cast<const uint32_t*>(kc + row)[j];
+        vr[u][j] = reinterpret_cast<const uint32_t*>(vc + row)[j];
+      }
+      kscale[u] = ks[key];
+      vscale[u] = vs[key];
+      on[u] = valid ? valid[key] : 1;
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = o[j] * corr + p * sv * vx[j];
-    m = mn;
+    for (int u = 0; u < U; ++u) {
+      const int key = key0 + u * NG;
+      float kx[8], vx[8], s = 0.f;
+      codes(kr[u], kx);
+      codes(vr[u], vx);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(q[j], kx[j], s);
+      s *= bf16_value(kscale[u]);
+#pragma unroll
+      for (int off = G / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+      if (key >= k1 || !on[u]) continue;       // the same for the whole lane group
+      s = modify_score(s * a.scores.scale, a.scores.softcap, slope, static_cast<float>(qpos - key));
+      const float mn = fmaxf(m, s), sv = bf16_value(vscale[u]);
+      const float corr = m == mn ? 1.f : expf(m - mn), p = s == -INFINITY ? 0.f : expf(s - mn);
+      l = l * corr + p;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = o[j] * corr + p * sv * vx[j];
+      m = mn;
+    }
   }
 #pragma unroll
   for (int off = G; off < 64; off <<= 1) {
