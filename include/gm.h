@@ -236,6 +236,36 @@ typedef struct gm_stats {
  * GM_E_HIP on failure (*out is then NULL). */
 int gm_model_create(const gm_config *cfg, const gm_weights *w, gm_model **out);
 
+/* Attention options of a model (gm_model_create_ex); zeros are the plain model.
+ *  kv_bits  8 or 4: with kv_cache, the cache holds k and v quantised
+ *           (gm_kv_cache); a decode step attends to the quantised rows, its own
+ *           token's included, a forward to the unquantised ones it computes.
+ *           0: the cache holds them in act_dtype.
+ *  softcap  > 0: scores become softcap * tanh(score / softcap).
+ *  slopes   device fp32 [n_heads], copied: scores less slopes[h] * |distance|
+ *           (ALiBi-style), next to whatever positions the model has; or NULL.
+ * Not for encoder-decoder models. */
+typedef struct gm_attn_options {
+  int32_t kv_bits;
+  float softcap;
+  const float* slopes;
+} gm_attn_options;
+
+/* gm_model_create with attention options (opts NULL: none). */
+int gm_model_create_ex(const gm_config *cfg, const gm_weights *w, const gm_attn_options *opts,
+                       gm_model **out);
+
+/* Documents and prefixes of the prompts of every later forward, which must be
+ * over B sequences of S tokens (GM_E_INVAL otherwise; decode steps are not
+ * affected by the shape): a token attends only to tokens of its own document
+ * (doc_ids, device int32 [B, S], or NULL: one document), and in a causal model
+ * also to later tokens before prefix[b] (device int32 [B], or NULL).  Positions
+ * stay 0 .. S - 1 over the whole row.  After a prefill of documents, decode steps
+ * continue the document of the last unmasked token.  The arrays are read by each
+ * forward when it runs and stay the caller's; 16-byte aligned.  Both NULL removes
+ * them.  Synchronises the device and drops the cached graphs. */
+int gm_set_segments(gm_model *m, const int32_t *doc_ids, const int32_t *prefix, int32_t B, int32_t S);
+
 /* Release everything the model owns.  Synchronises the device first.  NULL
  * is ignored. */
 void gm_model_destroy(gm_model *m);
@@ -500,6 +530,11 @@ typedef struct gm_cached_attention {
 int gm_attention_cached(const gm_cached_attention* a, hipStream_t stream);
 uint64_t gm_attention_cached_workspace(const gm_kv_cache* cache, int32_t dtype, int32_t B,
                                        int32_t Sq, int32_t n_heads);
+
+/* The cache of one layer of a model with kv_bits, for gm_kv_read (handing a
+ * sequence over, inspection) and gm_kv_write (taking one over).  It lives as long
+ * as the model; a forward or decode step in flight on another stream races. */
+int gm_model_kv_cache(const gm_model *m, int32_t layer, gm_kv_cache *out);
 
 /* Attention over whole prompts.  Query i of a sequence is at position
  * i + q_offset, key j at position j.  Query i sees key j when all of these

@@ -9,6 +9,7 @@
 
 #include "gm_device.h"
 #include "gm_kernels.h"
+#include "gm_ops.h"
 
 namespace gm {
 
@@ -22,7 +23,7 @@ constexpr int kDecPrologueThreads = 256;
 __global__ __launch_bounds__(kDecPrologueThreads) void k_decode_prologue(
     const int32_t* __restrict__ ids, int B, int vocab, int max_seq, int rotary, int capacity,
     int n_sites, const int32_t* __restrict__ seqlen, int32_t* __restrict__ pos,
-    int32_t* __restrict__ state) {
+    int32_t* __restrict__ state, int32_t* __restrict__ len, int32_t* __restrict__ live) {
   __shared__ uint32_t red_trap[kDecPrologueThreads / 64];
   __shared__ int red_need[kDecPrologueThreads / 64];
   const int tid = threadIdx.x;
@@ -40,6 +41,7 @@ __global__ __launch_bounds__(kDecPrologueThreads) void k_decode_prologue(
     if (p >= max_seq) trap = min(trap, (4u << 24) | static_cast<uint32_t>(b));
     need = max(need, p + 1);
     pos[b] = p < max_seq ? p : max_seq - 1;   // in bounds even when trapped
+    if (len) len[b] = (p < max_seq ? p : max_seq - 1) + 1;
   }
   for (int o = 32; o > 0; o >>= 1) {
     trap = min(trap, static_cast<uint32_t>(__shfl_xor(static_cast<int>(trap), o, 64)));
@@ -74,14 +76,20 @@ __global__ __launch_bounds__(kDecPrologueThreads) void k_decode_prologue(
     const int f = state[kFwdCount];
     state[kFwdIndex] = f;
     state[kFwdCount] = f + 1;
+    red_trap[0] = trap;
+  }
+  if (live) {
+    // a quantised cache stores a row of each sequence, or none after a failed guard
+    __syncthreads();
+    for (int b = tid; b < B; b += blockDim.x) live[b] = red_trap[0] == kTrapNone;
   }
 }
 
 void launch_decode_prologue(const int32_t* ids, int B, int vocab, int max_seq, int rotary,
                             int capacity, int n_sites, const int32_t* seqlen, int32_t* pos,
-                            int32_t* state, hipStream_t s) {
+                            int32_t* state, int32_t* len, int32_t* live, hipStream_t s) {
   hipLaunchKernelGGL(k_decode_prologue, dim3(1), dim3(kDecPrologueThreads), 0, s, ids, B, vocab,
-                     max_seq, rotary, capacity, n_sites, seqlen, pos, state);
+                     max_seq, rotary, capacity, n_sites, seqlen, pos, state, len, live);
 }
 
 // ------------------------------------------------------------ KV append
@@ -125,6 +133,23 @@ void launch_kv_store(const KvArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(k_kv_store, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a, vn);
 }
 
+// A prompt of several documents: only the last one's positions (the document of the
+// last unmasked token) stay valid for the tokens that continue it.
+__global__ __launch_bounds__(256) void k_kv_documents(uint8_t* valid, int stride, const int32_t* mask,
+                                                      const int32_t* docs, const int32_t* kv_len,
+                                                      int S) {
+  const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x, n = kv_len[b];
+  if (i >= S || n < 1) return;
+  const long long row = static_cast<long long>(b) * S;
+  valid[static_cast<long long>(b) * stride + i] = mask[row + i] != 0 && docs[row + i] == docs[row + n - 1];
+}
+
+void launch_kv_documents(uint8_t* valid, int stride, const int32_t* mask, const int32_t* docs,
+                         const int32_t* kv_len, int B, int S, hipStream_t s) {
+  hipLaunchKernelGGL(k_kv_documents, dim3((S + 255) / 256, B), dim3(256), 0, s, valid, stride, mask,
+                     docs, kv_len, S);
+}
+
 // ------------------------------------------------------------ attention
 // Split-key decode attention.  Workgroup (b*H + h, split) covers keys
 // [split*chunk, (split+1)*chunk) of sequence b up to its position pos[b]:
@@ -140,7 +165,8 @@ void launch_kv_store(const KvArgs& a, hipStream_t s) {
 // this GPU writes back the XCD's whole L2: far slower than the launch.)
 // Keys marked invalid get weight 0; a sequence without a valid key gets a
 // zero context.
-template <typename T, int HD>
+// MOD: the score goes through modify_score (a model with a cap or slopes).
+template <typename T, int HD, bool MOD>
 __global__ __launch_bounds__(1024) void k_decode_attn(DecAttnArgs a) {
   constexpr int NWV = 16;                      // wavefronts
   constexpr int VN = 16 / static_cast<int>(sizeof(T));
@@ -156,6 +182,8 @@ __global__ __launch_bounds__(1024) void k_decode_attn(DecAttnArgs a) {
   const int grp = lane / G, gl = lane % G;
   const int k0 = split * a.chunk;
   const int last = a.pos[b];
+  float slope = 0.f;
+  if constexpr (MOD) slope = a.slopes ? a.slopes[h] : 0.f;
 
   float q[VN];
   {
@@ -207,6 +235,7 @@ __global__ __launch_bounds__(1024) void k_decode_attn(DecAttnArgs a) {
       for (int off = G / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
       if (!(j0 + u * NG < k1 && vl[u])) continue;   // the same for the whole lane group
       s *= a.scale;
+      if constexpr (MOD) s = modify_score(s, a.softcap, slope, static_cast<float>(last - (j0 + u * NG)));
       const float mn = fmaxf(m, s);
       const float corr = expf(m - mn), p = expf(s - mn);
       const T* ve = reinterpret_cast<const T*>(&vr[u]);
@@ -285,7 +314,11 @@ __global__ __launch_bounds__(HD) void k_decode_combine(DecAttnArgs a) {
 
 template <typename T, int HD>
 static void decode_attn_t(const DecAttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_decode_attn<T, HD>), dim3(a.B * a.H, a.nsplit), dim3(1024), 0, s, a);
+  const dim3 grid(a.B * a.H, a.nsplit), block(1024);
+  if (a.softcap > 0.f || a.slopes)
+    hipLaunchKernelGGL((k_decode_attn<T, HD, true>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((k_decode_attn<T, HD, false>), grid, block, 0, s, a);
   if (a.nsplit > 1)
     hipLaunchKernelGGL((k_decode_combine<T, HD>), dim3(a.B * a.H), dim3(HD), 0, s, a);
 }

@@ -140,10 +140,12 @@ void launch_emit_effects(int32_t* state, void* fifo, int fifo_cap, int n_sites,
 // Guards and positions of one decode step (one workgroup): ids in [0, vocab)
 // (trap 1, index b), seqlen[b] < max_seq (trap 4, index b), rotary need =
 // max_b seqlen[b] + 1 <= capacity (trap 3); pos[b] = seqlen[b] (clamped);
-// rotary regrow as in the prologue; per-forward slots reset.
+// rotary regrow as in the prologue; per-forward slots reset.  A quantised cache
+// (len, live != null) also gets len[b] = pos[b] + 1, the keys of sequence b, and
+// live[b], 1 or after a failed guard 0, the rows it stores.
 void launch_decode_prologue(const int32_t* ids, int B, int vocab, int max_seq, int rotary,
                             int capacity, int n_sites, const int32_t* seqlen, int32_t* pos,
-                            int32_t* state, hipStream_t s);
+                            int32_t* state, int32_t* len, int32_t* live, hipStream_t s);
 
 struct KvArgs {
   int dtype;
@@ -159,6 +161,12 @@ struct KvArgs {
 };
 void launch_kv_store(const KvArgs& a, hipStream_t s);
 
+// After a prefill of several documents a sequence: the valid bytes (rows `stride`
+// apart) of the positions outside the last one become 0.  kv_len[b] = 1 + the last
+// unmasked position of sequence b.
+void launch_kv_documents(uint8_t* valid, int stride, const int32_t* mask, const int32_t* docs,
+                         const int32_t* kv_len, int B, int S, hipStream_t s);
+
 struct DecAttnArgs {
   int dtype;
   int B, H, hd, d;
@@ -169,6 +177,7 @@ struct DecAttnArgs {
   float* part;              // [B*H*nsplit*(hd+2)] partial softmax state per key chunk
   int nsplit, chunk;        // key chunks per head (1: no merge pass) and their size
   float scale;
+  float softcap; const float* slopes;   // > 0, [H]: modified scores (gm.h, gm_scores)
 };
 void launch_decode_attention(const DecAttnArgs& a, hipStream_t s);
 

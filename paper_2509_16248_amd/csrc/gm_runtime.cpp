@@ -15,6 +15,7 @@
 #include "gm_device.h"
 #include "gm_error.h"
 #include "gm_kernels.h"
+#include "gm_ops.h"
 
 namespace gm {
 void attention_set_order(int o);
@@ -135,6 +136,19 @@ struct gm_model {
   ArgmaxPart* argmax_parts = nullptr;
   int dec_nsplit = 0;
   int cache_B = 0;          // batch of the last prefill (host-side), 0 = none
+  // attention options (gm_model_create_ex): modified scores, and a cache in 8 or 4
+  // bits: per layer its memory (valid bytes shared), decode lengths, rows to
+  // store, and the workspace of the attention over it
+  float softcap = 0.f;
+  float* slopes = nullptr;
+  int kv_bits = 0;
+  std::vector<gm_kv_cache> qcache;
+  int32_t *dlen = nullptr, *dlive = nullptr;
+  void* cached_ws = nullptr;
+  uint64_t cached_ws_bytes = 0;
+  // documents and prefixes of the prompts (gm_set_segments) and their shape
+  const int32_t *seg_docs = nullptr, *seg_prefix = nullptr;
+  int seg_B = 0, seg_S = 0;
   // encoder-decoder (cfg.n_dec_layers > 0): decoder layers and their
   // cross-attention, encoder positions and final norm, the encoder output,
   // the cross queries, and k | v of every decoder layer projected from the
@@ -227,6 +241,35 @@ int validate(const gm_config* c) {
     if (c->rope_orig_max < 1) return inval("rope_orig_max must be positive");
     if (!(c->rope_attn_factor > 0.f)) return inval("rope_attn_factor must be positive");
   }
+  return GM_OK;
+}
+
+int validate_options(const gm_config& c, const gm_attn_options& o) {
+  if (o.kv_bits != 0 && o.kv_bits != 8 && o.kv_bits != 4) return inval("kv_bits must be 0, 8 or 4");
+  if (o.kv_bits && !c.kv_cache) return inval("kv_bits needs kv_cache");
+  if (!(o.softcap >= 0.f) || o.softcap > 3e38f) return inval("softcap must be finite and not negative");
+  if (c.n_dec_layers && (o.kv_bits || o.softcap > 0.f || o.slopes))
+    return inval("attention options are not supported with encoder-decoder models");
+  // sizes of a launch (gm_kv_write, gm_attention)
+  const double tokens = static_cast<double>(c.max_batch) * c.max_seq;
+  if (o.kv_bits && tokens * c.d_model / 4 >= 4294967040.0)
+    return inval("max_batch * max_seq * d_model / 4 must be below 2^32 - 256 with kv_bits");
+  return GM_OK;
+}
+
+// Workgroups of gm_attention over B sequences of S tokens fit one launch.
+int check_prompt_size(const gm_config& c, int B, int S) {
+  if (static_cast<double>(B) * c.n_heads * ((S + 31) / 32) >= 16777216.0)
+    return inval("B * n_heads * ceil(S / 32) must be below 2^24 with modified scores");
+  return GM_OK;
+}
+
+// What a forward over B sequences of S tokens needs of the attention options.
+int check_segments(const gm_model* m, int B, int S) {
+  const bool segs = m->seg_docs || m->seg_prefix;
+  if (segs && (B != m->seg_B || S != m->seg_S))
+    return inval("gm_set_segments was called for another B and S");
+  if (segs || m->softcap > 0.f || m->slopes) return check_prompt_size(m->cfg, B, S);
   return GM_OK;
 }
 
@@ -396,7 +439,7 @@ void enqueue(gm_model* m, int B, int S, const int32_t* ids, const int32_t* mask,
   if (prof) prof->start();
   if (dec)
     launch_decode_prologue(ids, B, c.vocab, c.max_seq, c.pos == GM_POS_ROTARY, c.rope_capacity,
-                           ns, m->seqlen, m->dpos, m->state, s);
+                           ns, m->seqlen, m->dpos, m->state, m->dlen, m->dlive, s);
   else if (on())
     launch_prologue(ids, mask, B, S, c.vocab, c.pos == GM_POS_ROTARY, c.rope_capacity, ns,
                     m->guard_expected, m->guard_B == B && m->guard_S == S, m->log_stage,
@@ -478,7 +521,7 @@ void enqueue(gm_model* m, int B, int S, const int32_t* ids, const int32_t* mask,
       q.norm_b = norm->b;
       q.norm_eps = c.norm_eps;
     }
-    if (dec && kind == GM_K_GEMM_QKV) {
+    if (dec && kind == GM_K_GEMM_QKV && !m->kv_bits) {
       // a decode step stores this layer's new k and v from the epilogue
       q.kc = m->kc[cur_layer];
       q.vc = m->vc[cur_layer];
@@ -578,8 +621,58 @@ void enqueue(gm_model* m, int B, int S, const int32_t* ids, const int32_t* mask,
     da.nsplit = (c.max_seq + da.chunk - 1) / da.chunk;
   }
   da.scale = at.scale;
+  da.softcap = m->softcap;
+  da.slopes = m->slopes;
+  // rows of q, k, v and ctx as operator tensors
+  const gm_scores scores{at.scale, m->softcap, m->slopes};
+  auto rows = [&](char* p, int width) {
+    return gm_tensor{p, static_cast<int64_t>(S) * width, width, hd};
+  };
+  char* kk = qq + d * m->esz;
+  char* vv = kk + d * m->esz;
+  const bool modified = m->softcap > 0.f || m->slopes || (!dec && (m->seg_docs || m->seg_prefix));
+  gm_prompt_attention pa{};
+  pa.dtype = m->dtype;
+  pa.B = B;
+  pa.Sq = pa.Sk = S;
+  pa.n_heads = pa.kv_heads = c.n_heads;
+  pa.head_dim = hd;
+  pa.q = rows(qq, 3 * d);
+  pa.k = rows(kk, 3 * d);
+  pa.v = rows(vv, 3 * d);
+  pa.out = rows(cc, d);
+  pa.causal = c.causal;
+  pa.scores = scores;
+  pa.key_mask = mask;
+  pa.q_doc = pa.k_doc = m->seg_docs;
+  pa.prefix = m->seg_prefix;
   auto attention = [&]() {
-    if (c.kv_cache && !dec) {
+    if (m->kv_bits && (dec || on())) {
+      // this layer's k and v, quantised
+      const gm_kv_cache& qcache = m->qcache[cur_layer];
+      launch_kv_write(qcache, m->dtype, B, S, rows(kk, 3 * d), rows(vv, 3 * d),
+                      dec ? m->dpos : nullptr, dec ? m->dlive : nullptr, dec ? nullptr : mask, s);
+    }
+    if (m->kv_bits) P(GM_K_KV_STORE, cur_layer, 0.0, 2.0 * T * d * (es + m->kv_bits / 8.0));
+    if (m->kv_bits && dec) {
+      gm_cached_attention ca{};
+      ca.cache = &m->qcache[cur_layer];
+      ca.dtype = m->dtype;
+      ca.B = B;
+      ca.Sq = 1;
+      ca.n_heads = c.n_heads;
+      ca.q = rows(qq, 3 * d);
+      ca.out = rows(cc, d);
+      ca.lengths = m->dlen;
+      ca.scores = scores;
+      ca.workspace = m->cached_ws;
+      ca.workspace_bytes = m->cached_ws_bytes;
+      launch_attention_cached(ca, s);
+      const double keys = static_cast<double>(B) * c.max_seq;   // upper bound: full cache
+      P(GM_K_ATTENTION, cur_layer, 4.0 * hd * keys * c.n_heads, 2.0 * keys * d * m->kv_bits / 8.0);
+      return;
+    }
+    if (c.kv_cache && !dec && !m->kv_bits) {
       // this layer's k and v go to the cache (a decode step stores them from
       // the QKV epilogue)
       kv.kc = m->kc[cur_layer];
@@ -595,7 +688,10 @@ void enqueue(gm_model* m, int B, int S, const int32_t* ids, const int32_t* mask,
       P(GM_K_ATTENTION, cur_layer, 4.0 * hd * keys * c.n_heads, es * 2.0 * keys * d);
       return;
     }
-    if (on()) launch_attention(at, s);
+    if (on()) {
+      if (modified) launch_attention_prompt(pa, s);
+      else launch_attention(at, s);
+    }
     P(GM_K_ATTENTION, cur_layer, attn_flops, attn_bytes);
   };
   // A pre-norm and the product that reads it: one launch for a few rows, two
@@ -650,6 +746,12 @@ void enqueue(gm_model* m, int B, int S, const int32_t* ids, const int32_t* mask,
     }
   }
   cur_layer = -1;
+  if (c.kv_cache && !dec && m->seg_docs) {
+    if (on())
+      launch_kv_documents(m->kv_valid, m->kv_bits ? m->qcache[0].max_seq : c.max_seq, mask, m->seg_docs,
+                          m->state + kKvLenBase, B, S, s);
+    P(GM_K_KV_STORE, -1, 0.0, 9.0 * T);
+  }
   if (pre)
     norm_gemm(GM_K_GEMM_HEAD, m->lnf_g, m->lnf_b, prev_site, m->head, c.vocab, kEpiStore, nullptr,
               logits, c.vocab);
@@ -942,10 +1044,17 @@ void gm_model_destroy(gm_model* m) {
 }
 
 int gm_model_create(const gm_config* cfg, const gm_weights* w, gm_model** out) {
+  return gm_model_create_ex(cfg, w, nullptr, out);
+}
+
+int gm_model_create_ex(const gm_config* cfg, const gm_weights* w, const gm_attn_options* opts,
+                       gm_model** out) {
   if (!out) return inval("out is NULL");
   *out = nullptr;
   int rc = validate(cfg);
   if (rc) return rc;
+  const gm_attn_options opt = opts ? *opts : gm_attn_options{};
+  if ((rc = validate_options(*cfg, opt))) return rc;
   if (!w || !w->layers) return inval("weights or weights->layers is NULL");
   const gm_config& c = *cfg;
   const bool ln = c.norm == GM_NORM_LAYER;
@@ -1124,15 +1233,18 @@ int gm_model_create(const gm_config* cfg, const gm_weights* w, gm_model** out) {
     return fail(rc);
   if (c.kv_cache) {
     const size_t per_layer = static_cast<size_t>(c.max_batch) * c.max_seq * d * es;
+    const int kv_rows = opt.kv_bits ? (c.max_seq + 63) / 64 * 64 : c.max_seq;   // positions held
     m->kc.assign(c.n_layers, nullptr);
     m->vc.assign(c.n_layers, nullptr);
-    for (int l = 0; l < c.n_layers; ++l)
-      if ((rc = m->alloc(&m->kc[l], per_layer)) || (rc = m->alloc(&m->vc[l], per_layer)))
-        return fail(rc);
+    if (!opt.kv_bits)
+      for (int l = 0; l < c.n_layers; ++l)
+        if ((rc = m->alloc(&m->kc[l], per_layer)) || (rc = m->alloc(&m->vc[l], per_layer)))
+          return fail(rc);
     // at most 32 key chunks per head (the workspace bound)
     m->dec_nsplit = 32;
     void* q = nullptr;
-    if ((rc = m->alloc(&q, static_cast<size_t>(c.max_batch) * c.max_seq))) return fail(rc);
+    const size_t valid_bytes = static_cast<size_t>(c.max_batch) * kv_rows;
+    if ((rc = m->alloc(&q, valid_bytes))) return fail(rc);
     m->kv_valid = static_cast<uint8_t*>(q);
     if ((rc = m->alloc(&q, c.max_batch * sizeof(int32_t)))) return fail(rc);
     m->seqlen = static_cast<int32_t*>(q);
@@ -1145,10 +1257,45 @@ int gm_model_create(const gm_config* cfg, const gm_weights* w, gm_model** out) {
     if ((rc = m->alloc(&q, static_cast<size_t>(c.max_batch) * kArgmaxParts * sizeof(ArgmaxPart))))
       return fail(rc);
     m->argmax_parts = static_cast<ArgmaxPart*>(q);
-    e = hipMemset(m->kv_valid, 0, static_cast<size_t>(c.max_batch) * c.max_seq);
+    e = hipMemset(m->kv_valid, 0, valid_bytes);
     if (e == hipSuccess) e = hipMemset(m->seqlen, 0, c.max_batch * sizeof(int32_t));
     if (e == hipSuccess) e = hipMemset(m->dpos, 0, c.max_batch * sizeof(int32_t));
     if (e != hipSuccess) return fail(hip_fail(e, "hipMemset"));
+      if (opt.kv_bits) {
+      m->kv_bits = opt.kv_bits;
+      const size_t codes = static_cast<size_t>(c.max_batch) * kv_rows * d * opt.kv_bits / 8;
+      const size_t scales = static_cast<size_t>(c.max_batch) * kv_rows * (d / kKvGroup) * 2;
+      for (int l = 0; l < c.n_layers; ++l) {
+        gm_kv_cache qc{opt.kv_bits, c.max_batch, c.n_heads, kv_rows, hd, nullptr, nullptr, nullptr,
+                       nullptr, m->kv_valid};
+        if ((rc = m->alloc(&qc.k, codes)) || (rc = m->alloc(&qc.v, codes)) ||
+            (rc = m->alloc(&qc.k_scale, scales)) || (rc = m->alloc(&qc.v_scale, scales)))
+          return fail(rc);
+        // positions never written read as zeros
+        if ((e = hipMemset(qc.k_scale, 0, scales)) != hipSuccess ||
+            (e = hipMemset(qc.v_scale, 0, scales)) != hipSuccess)
+          return fail(hip_fail(e, "hipMemset"));
+        m->qcache.push_back(qc);
+      }
+      if ((rc = m->alloc(&q, c.max_batch * sizeof(int32_t)))) return fail(rc);
+      m->dlen = static_cast<int32_t*>(q);
+      if ((rc = m->alloc(&q, c.max_batch * sizeof(int32_t)))) return fail(rc);
+      m->dlive = static_cast<int32_t*>(q);
+      // (fewer sequences split their keys further)
+      for (int b = 1; b <= c.max_batch; ++b) {
+        const uint64_t n = attention_cached_workspace(m->qcache[0], m->dtype, b, 1, c.n_heads);
+        m->cached_ws_bytes = n > m->cached_ws_bytes ? n : m->cached_ws_bytes;
+      }
+      if ((rc = m->alloc(&m->cached_ws, m->cached_ws_bytes))) return fail(rc);
+    }
+  }
+  m->softcap = opt.softcap;
+  if (opt.slopes) {
+    void* q = nullptr;
+    if ((rc = m->alloc(&q, c.n_heads * sizeof(float)))) return fail(rc);
+    m->slopes = static_cast<float*>(q);
+    e = hipMemcpy(q, opt.slopes, c.n_heads * sizeof(float), hipMemcpyDeviceToDevice);
+    if (e != hipSuccess) return fail(hip_fail(e, "slopes"));
   }
   // device state (encoder-decoder: the target's key lengths follow the source's)
   m->n_state = kKvLenBase + 2 * c.max_batch;
@@ -1335,6 +1482,7 @@ int gm_forward_ex(gm_model* m, int32_t B, int32_t S, const int32_t* ids, const i
   if (B < 1 || B > m->cfg.max_batch || S < 1 || S > m->cfg.max_seq)
     return inval("B or S out of range");
   if (m->cfg.n_dec_layers) return inval("an encoder-decoder model runs gm_forward_seq2seq");
+  if (int rc = check_segments(m, B, S)) return rc;
   m->stats.forwards++;
   if (m->cfg.kv_cache) m->cache_B = B;   // the forward fills the cache for these B sequences
   if (m->exec_mode == GM_EXEC_FRAGMENTED)
@@ -1434,6 +1582,7 @@ int gm_profile_forward(gm_model* m, int32_t B, int32_t S, const int32_t* ids,
     return inval("ids, mask and logits must be 16-byte aligned");
   if (B < 1 || B > m->cfg.max_batch || S < 1 || S > m->cfg.max_seq)
     return inval("B or S out of range");
+  if (int bad = check_segments(m, B, S)) return bad;
   Prof prof;
   prof.s = stream;
   enqueue(m, B, S, ids, mask, logits, stream, &prof);
@@ -1466,6 +1615,7 @@ int gm_debug_forward_layers(gm_model* m, int32_t B, int32_t S, const int32_t* id
        reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(dump)) & 15)
     return inval("ids, mask, logits and dump must be 16-byte aligned");
   if (B < 1 || B > c.max_batch || S < 1 || S > c.max_seq) return inval("B or S out of range");
+  if (int rc = check_segments(m, B, S)) return rc;
   Dump d;
   d.base = static_cast<char*>(dump);
   d.esz = m->esz;
@@ -1491,6 +1641,7 @@ int gm_forward_noalloc(gm_model* m, int32_t B, int32_t S, const int32_t* ids,
        reinterpret_cast<uintptr_t>(logits)) & 15)
     return inval("ids, mask and logits must be 16-byte aligned");
   if (B < 1 || B > c.max_batch || S < 1 || S > c.max_seq) return inval("B or S out of range");
+  if (int rc = check_segments(m, B, S)) return rc;
   // workspace: h, a, qkv, ctx, f (and tmp for post-norm models), each
   // rounded up to 256 bytes, carved from the static scratch array
   const size_t T = static_cast<size_t>(B) * S, d = c.d_model, es = m->esz;
@@ -1600,17 +1751,47 @@ int gm_flush_effects(gm_model* m, gm_effect_cb cb, void* user, int32_t* n_droppe
   return GM_OK;
 }
 
-int gm_set_mask_guard(gm_model* m, const int32_t* expected, int32_t B, int32_t S) {
-  if (!m) return inval("model is NULL");
-  if (expected && (B < 1 || S < 1)) return inval("expected mask shape must be positive");
-  if (reinterpret_cast<uintptr_t>(expected) & 15) return inval("expected must be 16-byte aligned");
+// Waits for the device and drops the captured graphs (they hold what is to change).
+static int drop_graphs(gm_model* m) {
   HIP_TRY(hipDeviceSynchronize());
-  // captured graphs hold the previous guard: drop them
   for (auto& g : m->graphs) HIP_TRY(hipGraphExecDestroy(g.exec));
   m->graphs.clear();
   for (auto& f : m->frags)
     for (hipGraphExec_t e : f.execs) HIP_TRY(hipGraphExecDestroy(e));
   m->frags.clear();
+  return GM_OK;
+}
+
+int gm_set_segments(gm_model* m, const int32_t* doc_ids, const int32_t* prefix, int32_t B, int32_t S) {
+  if (!m) return inval("model is NULL");
+  const bool some = doc_ids || prefix;
+  if (m->cfg.n_dec_layers) return inval("segments are not supported with encoder-decoder models");
+  if (some && (B < 1 || B > m->cfg.max_batch || S < 1 || S > m->cfg.max_seq))
+    return inval("B or S out of range");
+  if (prefix && !m->cfg.causal) return inval("prefix needs a causal model");
+  if ((reinterpret_cast<uintptr_t>(doc_ids) | reinterpret_cast<uintptr_t>(prefix)) & 15)
+    return inval("doc_ids and prefix must be 16-byte aligned");
+  if (int rc = drop_graphs(m)) return rc;
+  m->seg_docs = doc_ids;
+  m->seg_prefix = prefix;
+  m->seg_B = some ? B : 0;
+  m->seg_S = some ? S : 0;
+  return GM_OK;
+}
+
+int gm_model_kv_cache(const gm_model* m, int32_t layer, gm_kv_cache* out) {
+  if (!m || !out) return inval("NULL argument");
+  if (!m->kv_bits) return inval("the model was created without kv_bits");
+  if (layer < 0 || layer >= m->cfg.n_layers) return inval("layer out of range");
+  *out = m->qcache[layer];
+  return GM_OK;
+}
+
+int gm_set_mask_guard(gm_model* m, const int32_t* expected, int32_t B, int32_t S) {
+  if (!m) return inval("model is NULL");
+  if (expected && (B < 1 || S < 1)) return inval("expected mask shape must be positive");
+  if (reinterpret_cast<uintptr_t>(expected) & 15) return inval("expected must be 16-byte aligned");
+  if (int rc = drop_graphs(m)) return rc;
   m->guard_expected = expected;
   m->guard_B = expected ? B : 0;
   m->guard_S = expected ? S : 0;

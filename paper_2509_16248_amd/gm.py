@@ -123,6 +123,10 @@ class gm_prompt_attention(ctypes.Structure):
                 ("prefix", _vp)]
 
 
+class gm_attn_options(ctypes.Structure):
+    _fields_ = [("kv_bits", _i32), ("softcap", _f32), ("slopes", _vp)]
+
+
 KERNEL_KINDS = ["prologue", "rope_fill", "embed", "norm", "gemm_qkv", "attention",
                 "gemm_o", "gemm_up", "gemm_down", "gemm_head", "effects", "kv_store",
                 "argmax", "log", "gemm_xq", "gemm_xkv", "gemm_xo", "xattn"]
@@ -135,7 +139,7 @@ EXPORTS = ["gm_model_create", "gm_model_destroy", "gm_forward", "gm_forward_ex",
            "gm_check_error", "gm_flush_effects", "gm_debug_buffer", "gm_debug_forward_layers",
            "gm_get_stats", "gm_forward_noalloc",
            "gm_kv_write", "gm_kv_read", "gm_attention_cached", "gm_attention_cached_workspace",
-           "gm_attention",
+           "gm_attention", "gm_model_create_ex", "gm_set_segments", "gm_model_kv_cache",
            "gm_strerror",
            "gm_last_error"]
 
@@ -174,6 +178,10 @@ def lib(path: str = LIB_PATH) -> ctypes.CDLL:
     L.gm_debug_buffer.argtypes = [_vp, _i32, ctypes.POINTER(_vp), ctypes.POINTER(_u64)]
     L.gm_debug_forward_layers.argtypes = [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _u64]
     L.gm_get_stats.argtypes = [_vp, ctypes.POINTER(gm_stats)]
+    L.gm_model_create_ex.argtypes = [ctypes.POINTER(gm_config), ctypes.POINTER(gm_weights),
+                                     ctypes.POINTER(gm_attn_options), ctypes.POINTER(_vp)]
+    L.gm_set_segments.argtypes = [_vp, _vp, _vp, _i32, _i32]
+    L.gm_model_kv_cache.argtypes = [_vp, _i32, ctypes.POINTER(gm_kv_cache)]
     L.gm_kv_write.argtypes = [ctypes.POINTER(gm_kv_cache), _i32, _i32, _i32, gm_tensor, gm_tensor,
                               _vp, _vp, _vp, _vp]
     L.gm_kv_read.argtypes = [ctypes.POINTER(gm_kv_cache), _i32, _i32, _i32, _vp, _vp, gm_tensor,
@@ -214,6 +222,24 @@ def gm_model_create(cfg: gm_config, w: gm_weights) -> int:
     _check(lib().gm_model_create(ctypes.byref(cfg), ctypes.byref(w), ctypes.byref(out)),
            "gm_model_create")
     return out.value
+
+
+def gm_model_create_ex(cfg: gm_config, w: gm_weights, opts: Optional[gm_attn_options]) -> int:
+    out = _vp()
+    _check(lib().gm_model_create_ex(ctypes.byref(cfg), ctypes.byref(w),
+                                    None if opts is None else ctypes.byref(opts),
+                                    ctypes.byref(out)), "gm_model_create_ex")
+    return out.value
+
+
+def gm_set_segments(m: int, doc_ids: Optional[int], prefix: Optional[int], B: int, S: int) -> None:
+    _check(lib().gm_set_segments(m, doc_ids, prefix, B, S), "gm_set_segments")
+
+
+def gm_model_kv_cache(m: int, layer: int) -> gm_kv_cache:
+    c = gm_kv_cache()
+    _check(lib().gm_model_kv_cache(m, layer, ctypes.byref(c)), "gm_model_kv_cache")
+    return c
 
 
 def gm_model_destroy(m: int) -> None:

@@ -57,11 +57,16 @@ def torch_dtype(dtype: str) -> torch.dtype:
 
 class GmModel:
     """One libgm model.  ``globals_`` / ``layers`` hold host arrays (or
-    device tensors) named as in gm_weights / gm_layer_weights."""
+    device tensors) named as in gm_weights / gm_layer_weights.
+
+    Attention options (gm_attn_options): ``kv_bits`` 8 or 4 holds the KV cache
+    quantised, ``softcap`` > 0 caps the scores by a tanh, ``slopes`` (one number
+    per head) takes slope times distance off them."""
 
     def __init__(self, cfg, globals_: Dict, layers: List[Dict], device="cuda",
                  max_batch: Optional[int] = None, max_seq: Optional[int] = None,
-                 kv_cache: bool = False, dec_layers: Optional[List[Dict]] = None):
+                 kv_cache: bool = False, dec_layers: Optional[List[Dict]] = None,
+                 kv_bits: int = 0, softcap: float = 0.0, slopes=None):
         self.cfg = cfg
         self.device = torch.device(device)
         self.c = make_config(cfg, max_batch, max_seq, kv_cache)
@@ -112,9 +117,15 @@ class GmModel:
                 t = torch.as_tensor(np.asarray(x, dtype=np.float32)).to(self.device)
                 keep.append(t)
                 setattr(w, name, t.data_ptr())
+        opts = gm.gm_attn_options(kv_bits=kv_bits, softcap=softcap)
+        if slopes is not None:
+            t = torch.as_tensor(slopes, dtype=torch.float32).to(self.device).contiguous()
+            assert t.shape == (cfg.n_heads,)
+            keep.append(t)
+            opts.slopes = t.data_ptr()
         torch.cuda.synchronize(self.device)
         with torch.cuda.device(self.device):
-            self.handle = gm.gm_model_create(self.c, w)
+            self.handle = gm.gm_model_create_ex(self.c, w, opts)
         del keep
 
     def _stream(self, stream):
@@ -173,6 +184,32 @@ class GmModel:
                           next_ids.data_ptr() if next_ids is not None else None,
                           self._stream(stream))
         return logits
+
+    def set_segments(self, doc_ids: Optional[torch.Tensor] = None,
+                     prefix: Optional[torch.Tensor] = None, shape=None):
+        """Documents (int32 [B, S]) and prefixes (int32 [B], with ``shape`` (B, S)
+        when there are no documents) of the prompts of every later forward
+        (gm_set_segments; neither removes them).  Keeps references."""
+        for t in (doc_ids, prefix):
+            assert t is None or (t.dtype == torch.int32 and t.is_contiguous()
+                                 and t.is_cuda)
+        B, S = doc_ids.shape if doc_ids is not None else (shape or (0, 0))
+        assert prefix is None or prefix.shape == (B,)
+        gm.gm_set_segments(self.handle, doc_ids.data_ptr() if doc_ids is not None else None,
+                           prefix.data_ptr() if prefix is not None else None, B, S)
+        self._segments = (doc_ids, prefix)
+
+    def read_cache(self, layer: int, n: int, batch: Optional[int] = None, stream=None):
+        """k and v [B, n, n_heads, head_dim] of positions 0 .. n - 1 as the
+        quantised cache of a layer holds them (gm_kv_read; ``kv_bits`` models)."""
+        c = gm.gm_model_kv_cache(self.handle, layer)
+        B = c.batch if batch is None else batch
+        shape = (B, n, c.heads, c.head_dim)
+        k, v = (torch.empty(shape, dtype=_TORCH[self.cfg.dtype], device=self.device) for _ in "kv")
+        kt, vt = (gm.gm_tensor(t.data_ptr(), *t.stride()[:3]) for t in (k, v))
+        with torch.cuda.device(self.device):
+            gm.gm_kv_read(c, _DTYPES[self.cfg.dtype], B, n, None, None, kt, vt, self._stream(stream))
+        return k, v
 
     def new_decode_logits(self, B: int) -> torch.Tensor:
         return torch.empty((B, self.c.vocab), dtype=_TORCH[self.cfg.dtype], device=self.device)

@@ -165,3 +165,29 @@ def test_wrappers_refuse_host_tensors_and_bad_arguments():
         c.read(4, dtype=torch.int8)
     with pytest.raises(ValueError, match="batch"):
         c.read(4, batch=3)
+
+
+@pytest.mark.parametrize("name,over,opts,message", [
+    ("causal_lm_768", dict(kv_cache=1), dict(kv_bits=3), "kv_bits must be"),
+    ("causal_lm_768", {}, dict(kv_bits=8), "needs kv_cache"),
+    ("causal_lm_768", {}, dict(softcap=-1.0), "softcap"),
+    ("causal_lm_768", {}, dict(softcap=float("inf")), "softcap"),
+    ("seq2seq_768", {}, dict(softcap=5.0), "encoder-decoder"),
+    ("seq2seq_768", {}, dict(slopes=P), "encoder-decoder"),
+    ("decoder_4096", dict(kv_cache=1, max_batch=512, max_seq=32000), dict(kv_bits=4), "2^32"),
+])
+def test_model_option_refusals(name, over, opts, message):
+    import synth
+    from paper_2509_16248_amd.model import make_config
+    c = make_config(synth.preset(name))
+    for k, v in over.items():
+        setattr(c, k, v)
+    refused(lambda: gm.gm_model_create_ex(c, gm.gm_weights(), gm.gm_attn_options(**opts)), message)
+
+
+def test_segment_and_cache_entries_refuse_null():
+    L = gm.lib()
+    assert L.gm_set_segments(None, None, None, 1, 1) == gm.GM_E_INVAL
+    assert L.gm_model_kv_cache(None, 0, None) == gm.GM_E_INVAL
+    out = ctypes.c_void_p()
+    assert L.gm_model_create_ex(None, None, None, ctypes.byref(out)) == gm.GM_E_INVAL
