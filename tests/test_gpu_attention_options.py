@@ -67,9 +67,9 @@ class Oracle(OracleModel):
 
 
 CASES = [
-    ("tiny_decoder", dict(softcap=5.0)), ("tiny_decoder", dict(slopes=True)),
+    ("tiny_decoder", dict(softcap=0.005)), ("tiny_decoder", dict(slopes=True)),
     ("causal_lm_768", dict(softcap=20.0, slopes=True)), ("encoder_1024", dict(slopes=True)),
-    ("encoder_clamp_1024", dict(softcap=30.0)), ("decoder_4096", dict(softcap=10.0)),
+    ("encoder_clamp_1024", dict(softcap=30.0)), ("decoder_4096", dict(softcap=0.1)),
 ]
 
 
@@ -93,7 +93,7 @@ def test_forward_with_modified_scores(name, opts):
     # the options matter: the plain model's logits are further away than the tolerance allows
     moved = np.abs(res.logits_f64 - plain.logits_f64).max() / np.abs(plain.logits_f64).max()
     print(f"{name}: the options move the logits by {moved:.3g}", flush=True)
-    assert moved > 0
+    assert moved > TOL[cfg.dtype]
     assert m.check_error() == (0, 0) and m.stats()["host_syncs_in_forward"] == 0
     # the eager, fragmented and no-allocation forwards run the same kernels
     for mode in ("eager", "fragmented"):
@@ -145,9 +145,9 @@ def decode(m, toks):
     return f64(out)
 
 
-@pytest.mark.parametrize("name,opts", [("tiny_decoder", dict(softcap=5.0, slopes=True)),
+@pytest.mark.parametrize("name,opts", [("tiny_decoder", dict(softcap=0.005, slopes=True)),
                                        ("causal_lm_768", dict(slopes=True)),
-                                       ("decoder_4096", dict(softcap=10.0))])
+                                       ("decoder_4096", dict(softcap=0.1))])
 def test_decode_with_modified_scores_over_the_plain_cache(name, opts):
     cfg, w, o = setup(name, opts, 53)
     ids, mask = synth.make_inputs(cfg, 5, seq=12 if name == "tiny_decoder" else 100)
