@@ -498,7 +498,7 @@ int gm_kv_read(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n,
                const int32_t* start, const int32_t* count, gm_tensor k, gm_tensor v,
                hipStream_t stream);
 
-/* How a score is made from q.k.  scale multiplies it; then, with softcap > 0,
+/* How a score is made from q.k.  scale, positive, multiplies it; then, with softcap > 0,
  * s = softcap * tanh(s / softcap); then, with slopes (fp32 [n_heads] of the
  * query heads, or NULL), s -= slopes[h] * |query position - key position|. */
 typedef struct gm_scores {

@@ -236,6 +236,10 @@ void prompt_f32(const gm_prompt_attention& a, hipStream_t s) {
 // 32 bits of four consecutive int32, at any 4-byte address.
 typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
 
+// Caps up to which bf16 scores need no running maximum: exp2(score) and its sums stay
+// within 2^72 2^24 times the values, far from the ends of bf16 and fp32.
+constexpr float kFixedCap = 50.f;
+
 constexpr int kTileWords = 128;   // key tiles a workgroup keeps a bit for: 32 a word (262144 keys)
 
 // Workgroup = 128 queries of one (sequence, head), as k_flash (gm_attention.hip)
@@ -245,7 +249,8 @@ constexpr int kTileWords = 128;   // key tiles a workgroup keeps a bit for: 32 a
 // What the scores go through instead:
 //  CAP   softcap tanh(x / softcap) = C - 2 C / (exp2(x c2) + 1) in log2 units, C =
 //        softcap log2(e): two transcendental and three other instructions
-//  BIAS  one subtraction and one fma with the distance
+//  BIAS  a subtraction and a multiplication make the distance's share, from which the
+//        products' sums start (after a cap: a subtraction and an fma)
 //  masks a 64-bit word per lane and tile: key mask (a ballot of wavefront 0), causal
 //        and prefix bounds (shifts) and documents (32 comparisons where the tile or
 //        the wavefront's queries hold more than one); none at all for a tile that is
@@ -258,7 +263,7 @@ constexpr int kTileWords = 128;   // key tiles a workgroup keeps a bit for: 32 a
 // matrix product.  Such a product is never finite, so queries whose sums came out
 // not finite are computed again by prompt_row, which skips hidden keys; the loop
 // itself checks nothing.
-template <typename T, int HD, bool CAP, bool BIAS>
+template <typename T, int HD, bool CAP, bool BIAS, bool FIXED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void k_prompt_flash(gm_prompt_attention a) {
   constexpr int QB = 128, KB = 64, NW = 4;
@@ -323,7 +328,9 @@ void k_prompt_flash(gm_prompt_attention a) {
   constexpr float kLog2e = 1.4426950408889634f;
   const float c2 = CAP ? a.scores.scale * (2.f * kLog2e) / a.scores.softcap : a.scores.scale * kLog2e;
   const float capc = a.scores.softcap * kLog2e;
-  const float slope2 = BIAS && a.scores.slopes ? a.scores.slopes[h] * kLog2e : 0.f;
+  // the slope, negative, in the units of the scores it is added to: log2 units after a
+  // cap, q.k before the scale without one
+  const float slope1 = BIAS ? a.scores.slopes[h] * (CAP ? -kLog2e : -1.f / a.scores.scale) : 0.f;
 
   // documents of the wavefront's queries: this lane's, and whether all are one
   int qd = 0;
@@ -335,6 +342,30 @@ void k_prompt_flash(gm_prompt_attention a) {
   }
   const bool sparse = mk || kd;
   if (sparse) {
+    // 1024 keys a step, 4 keys a thread, up to 8 steps of loads in flight
+    constexpr int U = 8, STEP = 4 * 256;
+    const int top = kend < kTileWords * 32 * KB ? kend : kTileWords * 32 * KB;
+    i32x4 m[U], d[U];
+    auto fetch = [&](int k0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int key = k0 + u * STEP + 4 * static_cast<int>(threadIdx.x);
+        m[u] = i32x4{1, 1, 1, 1};
+        d[u] = i32x4{0, 0, 0, 0};
+        if (k0 + u * STEP >= top) break;
+        if (key + 4 <= S) {
+          if (mk) m[u] = *reinterpret_cast<const i32x4*>(mk + key);
+          if (kd) d[u] = *reinterpret_cast<const i32x4*>(kd + key);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            m[u][e] = key + e < S && (!mk || mk[key + e]);
+            if (kd && key + e < S) d[u][e] = kd[key + e];
+          }
+        }
+      }
+    };
+    fetch(0);
     int dmin = 0, dmax = 0;
     if (kd) {
       const int32_t* qds = a.q_doc + static_cast<long long>(b) * Sq;
@@ -351,38 +382,19 @@ void k_prompt_flash(gm_prompt_attention a) {
     }
     for (int i = threadIdx.x; i < kTileWords; i += 256) sTiles[i] = 0;
     __syncthreads();
-    const int top = kend < kTileWords * 32 * KB ? kend : kTileWords * 32 * KB;
-    // 256 keys (4 tiles) a step, 4 keys a lane, 4 steps of loads in flight
-    for (int k0 = wave * 1024; k0 < top; k0 += NW * 1024) {
-      i32x4 m[4], d[4];
+    for (int k0 = 0; k0 < top; k0 += U * STEP) {
+      if (k0) fetch(k0);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int key = k0 + 256 * u + 4 * lane;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m[u][e] = d[u][e] = 0;
-        if (key + 4 <= S) {
-          if (mk) m[u] = *reinterpret_cast<const i32x4*>(mk + key);
-          if (kd) d[u] = *reinterpret_cast<const i32x4*>(kd + key);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (mk && key + e < S) m[u][e] = mk[key + e];
-            if (kd && key + e < S) d[u][e] = kd[key + e];
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int key = k0 + 256 * u + 4 * lane;
+      for (int u = 0; u < U; ++u) {
+        if (k0 + u * STEP >= top) break;
         bool any = false;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          any |= key + e < S && (!mk || m[u][e] != 0) && (!kd || (d[u][e] >= dmin && d[u][e] <= dmax));
+        for (int e = 0; e < 4; ++e) any |= m[u][e] != 0 && d[u][e] >= dmin && d[u][e] <= dmax;
         const unsigned long long on = __ballot(any);
         uint32_t four = 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t) four |= ((on >> (16 * t)) & 0xffffull ? 1u : 0u) << t;
-        const int tile0 = (k0 + 256 * u) / KB;
+        const int tile0 = (k0 + u * STEP) / KB + 4 * wave;
         if (lane == 0 && four && tile0 < kTileWords * 32) atomicOr(&sTiles[tile0 / 32], four << (tile0 % 32));
       }
     }
@@ -466,10 +478,12 @@ void k_prompt_flash(gm_prompt_attention a) {
     }
     // ---- S^T = K Q^T: two 32-key blocks
     f32x16 sacc[2];
+    const float dist = static_cast<float>(qpos - kb - 4 * h2);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sacc[kk][i] = 0.f;
+      for (int i = 0; i < 16; ++i)
+        sacc[kk][i] = BIAS && !CAP ? slope1 * fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))) : 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
@@ -478,7 +492,7 @@ void k_prompt_flash(gm_prompt_attention a) {
         sacc[kk] = Mfma32A<T>::run(kf, qf[ks], sacc[kk]);
       }
     }
-    // ---- scores in log2 units
+    // ---- capped scores, in log2 units
     if constexpr (CAP) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
@@ -488,17 +502,13 @@ void k_prompt_flash(gm_prompt_attention a) {
           sacc[kk][i] = fmaf(-2.f * capc, __builtin_amdgcn_rcpf(e), capc);
         }
     }
-    if constexpr (BIAS) {
-      const float dist = static_cast<float>(qpos - kb - 4 * h2);
+    if constexpr (CAP && BIAS) {
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = CAP ? sacc[kk][i] : sacc[kk][i] * c2;
-          sacc[kk][i] = fmaf(-slope2, fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))), x);
-        }
+        for (int i = 0; i < 16; ++i)
+          sacc[kk][i] = fmaf(slope1, fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))), sacc[kk][i]);
     }
-    constexpr bool LOG2 = CAP || BIAS;          // already in log2 units
     // ---- masks
     const int last = qw0 + off > pre - 1 ? qw0 + off : pre - 1;
     if (bits != ~0ull || docs || (causal && kb + KB - 1 > last)) {
@@ -523,24 +533,27 @@ void k_prompt_flash(gm_prompt_attention a) {
           }
         }
     }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float mt = LOG2 ? mx : mx * c2;
-    if (__ballot(mt > mrun + kTau)) {          // move the maximum (wavefront-uniform)
-      const float mnew = fmaxf(mrun, mt);
-      const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
-      lrun *= alpha;
-#pragma unroll
-      for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
-      mrun = mnew;
-    }
     // fp16 probabilities times 2^7 (at most 2^15): fewer fall below its smallest normal
     constexpr float kUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
-    const float msub = mrun == -INFINITY ? 0.f : mrun - kUp;
+    float msub = 0.f;
+    if constexpr (!FIXED) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
+      float mt = CAP ? mx : mx * c2;
+      if (__ballot(mt > mrun + kTau)) {        // move the maximum (wavefront-uniform)
+        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+        const float mnew = fmaxf(mrun, mt);
+        const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+        lrun *= alpha;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
+        mrun = mnew;
+      }
+      msub = mrun == -INFINITY ? 0.f : mrun - kUp;
+    }
     // ---- probabilities, their sum, and P^T as 16-bit B operands
     vec pb[4];
 #pragma unroll
@@ -551,8 +564,8 @@ void k_prompt_flash(gm_prompt_attention a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float s0 = sacc[kk][8 * hf + 2 * j], s1 = sacc[kk][8 * hf + 2 * j + 1];
-          const float p0 = __builtin_amdgcn_exp2f(LOG2 ? s0 - msub : fmaf(s0, c2, -msub));
-          const float p1 = __builtin_amdgcn_exp2f(LOG2 ? s1 - msub : fmaf(s1, c2, -msub));
+          const float p0 = __builtin_amdgcn_exp2f(FIXED ? s0 : CAP ? s0 - msub : fmaf(s0, c2, -msub));
+          const float p1 = __builtin_amdgcn_exp2f(FIXED ? s1 : CAP ? s1 - msub : fmaf(s1, c2, -msub));
           lrun += p0 + p1;
           w[j] = pack2<T>(p0, p1);
         }
@@ -632,13 +645,19 @@ void k_prompt_flash(gm_prompt_attention a) {
 template <typename T, int HD>
 void prompt_flash(const gm_prompt_attention& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((a.Sq + 127) / 128) * a.n_heads * a.B), block(256);
-  const bool cap = a.scores.softcap > 0.f;
-  // without a cap the maximum is taken before the scale, which has to keep its order
-  const bool bias = a.scores.slopes || (!cap && !(a.scores.scale > 0.f));
-  if (cap && bias) hipLaunchKernelGGL((k_prompt_flash<T, HD, true, true>), grid, block, 0, s, a);
-  else if (cap) hipLaunchKernelGGL((k_prompt_flash<T, HD, true, false>), grid, block, 0, s, a);
-  else if (bias) hipLaunchKernelGGL((k_prompt_flash<T, HD, false, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_prompt_flash<T, HD, false, false>), grid, block, 0, s, a);
+  const bool cap = a.scores.softcap > 0.f, bias = a.scores.slopes;
+  auto launch = [&](auto c, auto b, auto fixed) {
+    hipLaunchKernelGGL((k_prompt_flash<T, HD, decltype(c)::value, decltype(b)::value, decltype(fixed)::value>),
+                       grid, block, 0, s, a);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if constexpr (std::is_same<T, bf16_t>::value)
+    if (cap && !bias && a.scores.softcap <= kFixedCap) return launch(yes, no, yes);
+  if (cap && bias) launch(yes, yes, no);
+  else if (cap) launch(yes, no, no);
+  else if (bias) launch(no, yes, no);
+  else launch(no, no, no);
 }
 
 }  // namespace

@@ -92,7 +92,7 @@ int check_rows(const gm_kv_cache* c, int dtype, int B, int n, const gm_tensor& k
 }
 
 int check_scores(const gm_scores& s) {
-  if (!std::isfinite(s.scale)) return inval("scale must be finite");
+  if (!(s.scale > 0.f) || !std::isfinite(s.scale)) return inval("scale must be positive and finite");
   if (!(s.softcap >= 0.f) || !std::isfinite(s.softcap))
     return inval("softcap must be finite and not negative (0: none)");
   if (misaligned(s.slopes, 4)) return inval("slopes must be 4-byte aligned");
