@@ -241,7 +241,7 @@ int gm_model_create(const gm_config *cfg, const gm_weights *w, gm_model **out);
  *           (gm_kv_cache); a decode step attends to the quantised rows, its own
  *           token's included, a forward to the unquantised ones it computes.
  *           0: the cache holds them in act_dtype.
- *  softcap  > 0: scores become softcap * tanh(score / softcap).
+ *  softcap  > 0 (1e-6 to 1024): scores become softcap * tanh(score / softcap).
  *  slopes   device fp32 [n_heads], copied: scores less slopes[h] * |distance|
  *           (ALiBi-style), next to whatever positions the model has; or NULL.
  * Not for encoder-decoder models. */
@@ -498,8 +498,8 @@ int gm_kv_read(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n,
                const int32_t* start, const int32_t* count, gm_tensor k, gm_tensor v,
                hipStream_t stream);
 
-/* How a score is made from q.k.  scale, positive, multiplies it; then, with softcap > 0,
- * s = softcap * tanh(s / softcap); then, with slopes (fp32 [n_heads] of the
+/* How a score is made from q.k.  scale, positive, multiplies it; then, with softcap > 0
+ * (1e-6 to 1024), s = softcap * tanh(s / softcap); then, with slopes (fp32 [n_heads] of the
  * query heads, or NULL), s -= slopes[h] * |query position - key position|. */
 typedef struct gm_scores {
   float scale, softcap;

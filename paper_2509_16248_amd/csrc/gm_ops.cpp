@@ -93,8 +93,8 @@ int check_rows(const gm_kv_cache* c, int dtype, int B, int n, const gm_tensor& k
 
 int check_scores(const gm_scores& s) {
   if (!(s.scale > 0.f) || !std::isfinite(s.scale)) return inval("scale must be positive and finite");
-  if (!(s.softcap >= 0.f) || !std::isfinite(s.softcap))
-    return inval("softcap must be finite and not negative (0: none)");
+  if (s.softcap != 0.f && !(s.softcap >= kLeastCap && s.softcap <= kLargestCap))
+    return inval("softcap must be 0 (none) or from 1e-6 to 1024");
   if (misaligned(s.slopes, 4)) return inval("slopes must be 4-byte aligned");
   return GM_OK;
 }

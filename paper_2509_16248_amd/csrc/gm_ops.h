@@ -12,6 +12,10 @@ namespace gm {
 
 constexpr int kKvGroup = 32;   // channels per scale of a quantised cache
 
+// Caps of scores.  The 16-bit kernels take softcap tanh(x) as softcap - 2 softcap /
+// (exp(2 x) + 1), off by 2^-23 softcap or so whatever x is: 1.2e-4 at the largest.
+constexpr float kLeastCap = 1e-6f, kLargestCap = 1024.f;
+
 void launch_kv_write(const gm_kv_cache& c, int dtype, int B, int n, const gm_tensor& k,
                      const gm_tensor& v, const int32_t* start, const int32_t* count,
                      const int32_t* mask, hipStream_t s);

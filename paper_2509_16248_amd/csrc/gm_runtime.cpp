@@ -247,7 +247,8 @@ int validate(const gm_config* c) {
 int validate_options(const gm_config& c, const gm_attn_options& o) {
   if (o.kv_bits != 0 && o.kv_bits != 8 && o.kv_bits != 4) return inval("kv_bits must be 0, 8 or 4");
   if (o.kv_bits && !c.kv_cache) return inval("kv_bits needs kv_cache");
-  if (!(o.softcap >= 0.f) || o.softcap > 3e38f) return inval("softcap must be finite and not negative");
+  if (o.softcap != 0.f && !(o.softcap >= kLeastCap && o.softcap <= kLargestCap))
+    return inval("softcap must be 0 (none) or from 1e-6 to 1024");
   if (c.n_dec_layers && (o.kv_bits || o.softcap > 0.f || o.slopes))
     return inval("attention options are not supported with encoder-decoder models");
   // sizes of a launch (gm_kv_write, gm_attention)

@@ -239,6 +239,61 @@ def test_prompt_masks(dtype, hd, name):
                 **masks(name, B, Sq, Sk))
 
 
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("f16", 32), ("f32", 32)])
+@pytest.mark.parametrize("S", [1, 2, 3, 4, 5, 62, 63, 64, 65, 67])
+def test_prompt_masks_of_short_rows(dtype, hd, S):
+    for name in ("pads", "mixed holes", "causal docs", "prefix pads"):
+        prompt_case(dtype, hd, 2, S, S, 2, 1, what=name, **masks(name, 2, S, S))
+
+
+@pytest.mark.parametrize("softcap", [1e-6, 0.5, 50.0, 50.5, 1024.0])
+def test_caps_from_the_smallest_to_the_largest(softcap):
+    for dtype in ("bf16", "f16"):
+        prompt_case(dtype, 64, 1, 100, 100, 2, 2, what=f"cap {softcap}", softcap=softcap, size=4.0)
+        cached_case(dtype, 8, 64, 1, 1, 2, 2, 100, [100], softcap=softcap, size=4.0)
+
+
+def test_prompt_keys_past_the_tile_marks():
+    """More keys than a workgroup keeps marks for (131072), masked and of several
+    documents on both sides of that."""
+    Sq, Sk = 130, 131072 + 5000
+    g = torch.Generator().manual_seed(3)
+    ids = (torch.arange(Sk) // 9000).int()[None]
+    q_doc = torch.randint(0, 16, (1, Sq), generator=g, dtype=torch.int32)
+    mask = (torch.rand((1, Sk), generator=g) < 0.9).int()
+    prompt_case("bf16", 64, 1, Sq, Sk, 1, 1, what="long", k_doc=ids, q_doc=q_doc, key_mask=mask)
+    prompt_case("bf16", 64, 1, Sq, Sk, 1, 1, what="long, causal", causal=True, key_mask=mask)
+
+
+def test_cached_very_long_sequences():
+    cached_case("bf16", 4, 64, 1, 2, 2, 1, 70001, [70001], alibi=True)
+    cached_case("f32", 8, 32, 1, 1, 1, 1, 70001, [69999])
+
+
+def test_capture_on_a_stream_given_to_the_call():
+    B, H, hd, n = 2, 4, 64, 3000
+    c = KvCache(B, H, n, hd, bits=8)
+    k = rows((B, n, H, hd), "bf16", 2).cuda()
+    q = rows((B, 1, H, hd), "bf16", 3).cuda()
+    lengths = ints([n, 500])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        c.write(k, k)
+        ops.cached_attention(q, c, lengths)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        out = ops.cached_attention(q, c, lengths, stream=s)
+        full = ops.attention(q, k, k, stream=s)
+    for L in ([1, 2], [3000, 2999]):
+        lengths.copy_(torch.tensor(L))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ops.cached_attention(q, c, lengths))
+        assert torch.equal(full, ops.attention(q, k, k))
+
+
 def test_prompt_many_documents_over_many_tiles():
     B, Sq, Sk = 1, 700, 1100
     prompt_case("bf16", 64, B, Sq, Sk, 4, 1, what="docs", causal=True, **{

@@ -93,6 +93,10 @@ def cached(**kw):
     (dict(lengths=None), "lengths"), (dict(scores=gm.gm_scores(float("nan"), 0.0, None)), "scale"),
     (dict(scores=gm.gm_scores(1.0, -1.0, None)), "softcap"),
     (dict(scores=gm.gm_scores(1.0, float("inf"), None)), "softcap"),
+    (dict(scores=gm.gm_scores(1.0, 1025.0, None)), "softcap"),
+    (dict(scores=gm.gm_scores(1.0, 1e-7, None)), "softcap"),
+    (dict(scores=gm.gm_scores(0.0, 0.0, None)), "scale"),
+    (dict(scores=gm.gm_scores(-1.0, 0.0, None)), "scale"),
     (dict(scores=gm.gm_scores(1.0, 0.0, P + 1)), "slopes"),
 ])
 def test_cached_attention_refusals(kw, message):
