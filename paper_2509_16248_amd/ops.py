@@ -13,6 +13,7 @@ tensors made on another stream have to be ready there.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import struct
@@ -80,26 +81,37 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _on(device, stream, call, tensors):
-    """call(stream handle) with the device current; on a stream given by the
-    caller, what the call allocates belongs to that stream, and the allocator
-    is told that tensors() are in use there."""
+@contextlib.contextmanager
+def _there(device, stream, *tensors):
+    """The device made current and, if one is given, the stream: what a call
+    allocates then belongs to it, and the allocator is told that the tensors are
+    in use there."""
     if stream is None:
-        if device.index == torch.cuda.current_device():
-            return call(_raw_stream(device.index))
         with torch.cuda.device(device):
-            return call(_raw_stream(device.index))
+            yield
+        return
     if stream.device != device:
         raise ValueError(f"the stream must be on {device}, not {stream.device}")
     with torch.cuda.stream(stream):
-        for t in tensors():
+        for t in tensors:
             if t is not None:
                 t.record_stream(stream)
-        return call(stream.cuda_stream)
+        yield
+
+
+def _elsewhere(device, stream) -> bool:
+    return stream is not None or device.index != torch.cuda.current_device()
 
 
 def _tensor(*fields) -> gm.gm_tensor:
     return gm.gm_tensor.from_buffer_copy(_TENSOR.pack(*fields))
+
+
+def _empty(like: torch.Tensor, shape) -> torch.Tensor:
+    """A new contiguous tensor of that shape."""
+    if like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like)      # (a third faster)
+    return torch.empty(shape, dtype=like.dtype, device=like.device)
 
 
 class KvCache:
@@ -135,6 +147,7 @@ class KvCache:
                                 self.v.data_ptr(), self.k_scale.data_ptr(),
                                 self.v_scale.data_ptr(),
                                 self.valid.data_ptr() if masked else None)
+        self._ref = ctypes.byref(self.c)
         self._workspace = {}      # bytes that attention needs, by dtype and shape of the queries
 
     def nbytes(self) -> int:
@@ -154,19 +167,22 @@ class KvCache:
         attention (a ``masked`` cache; without it every stored position may be
         attended)."""
         dtype, code, device = _first(k, "k")
-        B, n = k.shape[0], k.shape[1]
         if device != self.device:
             raise ValueError(f"the cache is on {self.device}, the rows on {device}")
+        if _elsewhere(device, stream):
+            with _there(device, stream, k, v, start, count, mask, *self._tensors()):
+                return self.write(k, v, start, count, mask)
+        B, n = k.shape[0], k.shape[1]
         if B > self.batch:
             raise ValueError(f"the rows' batch {B} exceeds the cache's {self.batch}")
         shape = (B, n, self.heads, self.head_dim)
-        kt = _tensor(*_rows(k, "k", shape, dtype, device))
-        vt = _tensor(*_rows(v, "v", shape, dtype, device))
-        st, ct = _ints(start, "start", (B,), device), _ints(count, "count", (B,), device)
-        mt = _ints(mask, "mask", (B, n), device)
-        _on(device, stream,
-            lambda s: gm.gm_kv_write(self.c, code, B, n, kt, vt, st, ct, mt, s),
-            lambda: (k, v, start, count, mask, *self._tensors()))
+        rc = gm.lib().gm_kv_write(
+            self._ref, code, B, n, _tensor(*_rows(k, "k", shape, dtype, device)),
+            _tensor(*_rows(v, "v", shape, dtype, device)), _ints(start, "start", (B,), device),
+            _ints(count, "count", (B,), device), _ints(mask, "mask", (B, n), device),
+            _raw_stream(device.index))
+        if rc:
+            raise gm.GmError(rc, "gm_kv_write")
 
     def read(self, n: int, start: Optional[torch.Tensor] = None,
              count: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
@@ -185,18 +201,20 @@ class KvCache:
         if not 0 <= B <= self.batch or n < 0:
             raise ValueError("batch must be at most the cache's, and n not negative")
         shape, device = (B, n, self.heads, self.head_dim), self.device
-        st, ct = _ints(start, "start", (B,), device), _ints(count, "count", (B,), device)
-
-        def call(s):
-            k, v = out if out is not None else (
-                torch.empty(shape, dtype=dtype, device=device),
-                torch.empty(shape, dtype=dtype, device=device))
-            kt = _tensor(*_rows(k, "k", shape, dtype, device))
-            vt = _tensor(*_rows(v, "v", shape, dtype, device))
-            gm.gm_kv_read(self.c, code, B, n, st, ct, kt, vt, s)
-            return k, v
-
-        return _on(device, stream, call, lambda: (start, count, *(out or ()), *self._tensors()))
+        if device.type != "cuda":
+            raise ValueError(f"the cache must be on a HIP device, not {device}")
+        if _elsewhere(device, stream):
+            with _there(device, stream, start, count, *(out or ()), *self._tensors()):
+                return self.read(n, start, count, dtype, out, batch)
+        k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=device),
+                                            torch.empty(shape, dtype=dtype, device=device))
+        rc = gm.lib().gm_kv_read(
+            self._ref, code, B, n, _ints(start, "start", (B,), device),
+            _ints(count, "count", (B,), device), _tensor(*_rows(k, "k", shape, dtype, device)),
+            _tensor(*_rows(v, "v", shape, dtype, device)), _raw_stream(device.index))
+        if rc:
+            raise gm.GmError(rc, "gm_kv_read")
+        return k, v
 
 
 def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
@@ -220,25 +238,27 @@ def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
                          f"{cache.batch} sequences and its head_dim {cache.head_dim}")
     if lengths is None:
         raise ValueError("lengths is missing")
-    qt, lt = _rows(q, "q", shape, dtype, device), _ints(lengths, "lengths", (B,), device)
-    sl = _ints(slopes, "slopes", (H,), device, torch.float32)
+    if _elsewhere(device, stream):
+        with _there(device, stream, q, out, lengths, slopes, *cache._tensors()):
+            return cached_attention(q, cache, lengths, softcap=softcap, slopes=slopes, scale=scale,
+                                    out=out)
     need = cache._workspace.get((code, B, Sq, H))
     if need is None:
         need = gm.gm_attention_cached_workspace(cache.c, code, B, Sq, H)
         cache._workspace[code, B, Sq, H] = need
-
-    def call(s):
-        res = torch.empty(shape, dtype=dtype, device=device) if out is None else out
-        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        a = gm.gm_cached_attention.from_buffer_copy(_CACHED.pack(
-            ctypes.addressof(cache.c), code, B, Sq, H, *qt,
-            *_rows(res, "out", shape, dtype, device), lt,
-            1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl,
-            work.data_ptr() if need else 0, need))
-        gm.gm_attention_cached(a, s)
-        return res
-
-    return _on(device, stream, call, lambda: (q, out, lengths, slopes, *cache._tensors()))
+    if out is None:
+        out = _empty(q, shape)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    a = gm.gm_cached_attention.from_buffer_copy(_CACHED.pack(
+        ctypes.addressof(cache.c), code, B, Sq, H, *_rows(q, "q", shape, dtype, device),
+        *_rows(out, "out", shape, dtype, device), _ints(lengths, "lengths", (B,), device),
+        1.0 / math.sqrt(hd) if scale is None else scale, softcap,
+        _ints(slopes, "slopes", (H,), device, torch.float32),
+        work.data_ptr() if need else 0, need))
+    rc = gm.lib().gm_attention_cached(ctypes.byref(a), _raw_stream(device.index))
+    if rc:
+        raise gm.GmError(rc, "gm_attention_cached")
+    return out
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False,
@@ -257,25 +277,28 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool
     query that sees nothing gives zeros.  Scores as in
     :func:`cached_attention`."""
     dtype, code, device = _first(q, "q")
-    _first(k, "k")
-    qs = q.shape
-    B, Sq, H, hd = qs
-    Sk, Hkv = k.shape[1], k.shape[2]
-    ks = (B, Sk, Hkv, hd)
-    qt, kt, vt = (_rows(q, "q", qs, dtype, device), _rows(k, "k", ks, dtype, device),
-                  _rows(v, "v", ks, dtype, device))
-    sl = _ints(slopes, "slopes", (H,), device, torch.float32)
-    masks = (_ints(key_mask, "key_mask", (B, Sk), device), _ints(q_doc, "q_doc", (B, Sq), device),
-             _ints(k_doc, "k_doc", (B, Sk), device), _ints(prefix, "prefix", (B,), device))
-
-    def call(s):
-        res = torch.empty(qs, dtype=dtype, device=device) if out is None else out
-        a = gm.gm_prompt_attention.from_buffer_copy(_PROMPT.pack(
-            code, B, Sq, Sk, H, Hkv, hd, *qt, *kt, *vt, *_rows(res, "out", qs, dtype, device),
-            bool(causal), Sk - Sq if q_offset is None else q_offset,
-            1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl, *masks))
-        gm.gm_attention(a, s)
-        return res
-
-    return _on(device, stream, call,
-               lambda: (q, k, v, out, slopes, key_mask, q_doc, k_doc, prefix))
+    if k.dim() != 4:
+        raise ValueError("k must be [batch, tokens, heads, head_dim]")
+    if _elsewhere(device, stream):
+        with _there(device, stream, q, k, v, out, slopes, key_mask, q_doc, k_doc, prefix):
+            return attention(q, k, v, causal=causal, softcap=softcap, slopes=slopes,
+                             key_mask=key_mask, q_doc=q_doc, k_doc=k_doc, prefix=prefix,
+                             q_offset=q_offset, scale=scale, out=out)
+    shape = q.shape
+    B, Sq, H, hd = shape
+    _, Sk, Hkv, _ = k.shape
+    keys = (B, Sk, Hkv, hd)
+    if out is None:
+        out = _empty(q, shape)
+    a = gm.gm_prompt_attention.from_buffer_copy(_PROMPT.pack(
+        code, B, Sq, Sk, H, Hkv, hd, *_rows(q, "q", shape, dtype, device),
+        *_rows(k, "k", keys, dtype, device), *_rows(v, "v", keys, dtype, device),
+        *_rows(out, "out", shape, dtype, device), bool(causal),
+        Sk - Sq if q_offset is None else q_offset, 1.0 / math.sqrt(hd) if scale is None else scale,
+        softcap, _ints(slopes, "slopes", (H,), device, torch.float32),
+        _ints(key_mask, "key_mask", (B, Sk), device), _ints(q_doc, "q_doc", (B, Sq), device),
+        _ints(k_doc, "k_doc", (B, Sk), device), _ints(prefix, "prefix", (B,), device)))
+    rc = gm.lib().gm_attention(ctypes.byref(a), _raw_stream(device.index))
+    if rc:
+        raise gm.GmError(rc, "gm_attention")
+    return out
