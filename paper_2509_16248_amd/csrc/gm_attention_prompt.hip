@@ -13,6 +13,8 @@ namespace gm {
 
 namespace {
 
+constexpr float kLog2e = 1.4426950408889634f;
+
 // One query by one wavefront, a key per lane: two passes over the keys, the
 // largest score, then the sums.  A key of weight 0 is skipped, so that nothing a
 // hidden value holds can reach the sums.
@@ -83,17 +85,18 @@ __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, 
 // finite are computed again by prompt_row: a hidden key's weight is 0, but its product
 // with an Inf or NaN value is not.
 template <int HD, bool CAP>
-__global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 3)))
+void k_prompt_f32(gm_prompt_attention a) {
   constexpr int NC = HD / 8, CB = HD / 32, NW = 4;
   typedef float f32x4a __attribute__((ext_vector_type(4)));
   __shared__ float s_m[NW][32], s_l[NW][32];
   __shared__ float s_o[NW][HD][33];
   __shared__ uint32_t s_odd[NW];
-  const int nqb = (a.Sq + 31) / 32;
-  int x = blockIdx.x;
-  const int qb = a.causal ? nqb - 1 - x % nqb : x % nqb;
-  x /= nqb;
-  const int h = x % a.n_heads, b = x / a.n_heads, kvh = h / (a.n_heads / a.kv_heads);
+  // order as in k_prompt_flash: query blocks outermost, heaviest first
+  const int nqb = (a.Sq + 31) / 32, P = a.B * a.n_heads, blk = blockIdx.x / P, pair = blockIdx.x - blk * P;
+  const int qb = a.causal ? nqb - 1 - blk : blk;
+  const int b = pair / a.n_heads, hp = pair - b * a.n_heads;
+  const int kvh = hp % a.kv_heads, h = kvh * (a.n_heads / a.kv_heads) + hp / a.kv_heads;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int l32 = lane & 31, g = lane >> 5;
   const int Sq = a.Sq, Sk = a.Sk, q0 = qb * 32, qi = q0 + l32, qpos = qi + a.q_offset;
@@ -104,7 +107,10 @@ __global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
   const int32_t* mk = a.key_mask ? a.key_mask + static_cast<long long>(b) * Sk : nullptr;
   const int32_t* kd = a.q_doc ? a.k_doc + static_cast<long long>(b) * Sk : nullptr;
   const int qd = a.q_doc ? a.q_doc[static_cast<long long>(b) * Sq + qc] : 0;
-  const float slope = a.scores.slopes ? a.scores.slopes[h] : 0.f;
+  // scores in log2 units
+  const float scale = CAP ? a.scores.scale / a.scores.softcap : a.scores.scale * kLog2e;
+  const float capc = a.scores.softcap * kLog2e;
+  const float slope = a.scores.slopes ? a.scores.slopes[h] * kLog2e : 0.f;
   const int pre = a.causal && a.prefix ? a.prefix[b] : 0;
   int kend = Sk;                               // keys this lane's query may see end here
   if (a.causal) {
@@ -142,14 +148,16 @@ __global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
     f32x4a kf[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const f32x4a*>(k + 8 * c);
-    float vf[16][CB];
+    // V rows, 32 channels at a time, one step ahead of the products
+    float vf[2][16];
+    auto fetch_v = [&](int c, float (&dst)[16]) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      const int key = k0 + 8 * (t / 4) + 4 * g + t % 4;
-      const float* v = vb + (key < Sk ? key : Sk - 1) * a.v.token + l32;
-#pragma unroll
-      for (int c = 0; c < CB; ++c) vf[t][c] = v[32 * c];
-    }
+      for (int t = 0; t < 16; ++t) {
+        const int key = k0 + 8 * (t / 4) + 4 * g + t % 4;
+        dst[t] = vb[(key < Sk ? key : Sk - 1) * a.v.token + l32 + 32 * c];
+      }
+    };
+    fetch_v(0, vf[0]);
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -158,20 +166,22 @@ __global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][r], qf[c][r], s, 0, 0, 0);
     float top = m;
+    const float dist = static_cast<float>(qpos - k0 - 4 * g);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int key = k0 + 8 * (e / 4) + 4 * g + e % 4;
-      const float y = modify_score(s[e] * a.scores.scale, CAP ? a.scores.softcap : 0.f, slope,
-                                   fabsf(static_cast<float>(qpos - key)));
+      float y = s[e] * scale;
+      if constexpr (CAP) y = capc * tanhf(y);
+      y = fmaf(-slope, fabsf(dist - static_cast<float>(8 * (e / 4) + e % 4)), y);
       s[e] = vis >> e & 1 ? y : -INFINITY;
       top = fmaxf(top, s[e]);
     }
     top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float corr = top == -INFINITY ? 1.f : expf(m - top);   // (m = -inf: 0)
+    const float corr = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);   // (m = -inf: 0)
+    const float msub = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      s[e] = s[e] == -INFINITY ? 0.f : expf(s[e] - top);
+      s[e] = __builtin_amdgcn_exp2f(s[e] - msub);
       sum += s[e];
     }
     l = l * corr + sum;
@@ -180,8 +190,9 @@ __global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
     for (int c = 0; c < CB; ++c) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[c][e] *= corr;
+      if (c + 1 < CB) fetch_v(c + 1, vf[(c + 1) % 2]);
 #pragma unroll
-      for (int t = 0; t < 16; ++t) o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[t][c], s[t], o[c], 0, 0, 0);
+      for (int t = 0; t < 16; ++t) o[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[c % 2][t], s[t], o[c], 0, 0, 0);
     }
   }
   l += __shfl_xor(l, 32, 64);
@@ -213,7 +224,7 @@ __global__ __launch_bounds__(256) void k_prompt_f32(gm_prompt_attention a) {
     if (M != -INFINITY)
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const float f = s_m[w][i] == -INFINITY ? 0.f : expf(s_m[w][i] - M);
+        const float f = s_m[w][i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][i] - M);
         L += s_l[w][i] * f;
         O += s_o[w][c][i] * f;
       }
@@ -336,7 +347,6 @@ void k_prompt_flash(gm_prompt_attention a) {
     kend = last > pre ? last : pre;
     kend = kend < S ? kend : S;
   }
-  constexpr float kLog2e = 1.4426950408889634f;
   const float c2 = CAP ? a.scores.scale * (2.f * kLog2e) / a.scores.softcap : a.scores.scale * kLog2e;
   const float capc = a.scores.softcap * kLog2e;
   // the slope, negative, in the units of the scores it is added to: log2 units after a
