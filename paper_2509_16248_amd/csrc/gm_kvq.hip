@@ -365,9 +365,13 @@ struct CachedPlace {
   int b, kvh, blk, split, len, k0, k1;
   __device__ __forceinline__ CachedPlace(const gm_cached_attention& a, const gm_kv_cache& c,
                                          const CachedPlan& p) {
+    // (heads fastest: the row blocks of a head come to one XCD where the heads are a
+    // multiple of 8, and share its L2: 4 sequences of 16000 keys, 32/2 heads of 128, 8 bits,
+    // 29.8 us with the blocks side by side, 25.9 so)
     int x = blockIdx.x;
-    blk = x % p.blocks;
-    x /= p.blocks;
+    const int heads = a.B * c.heads;
+    blk = x / heads;
+    x -= blk * heads;
     kvh = x % c.heads;
     b = x / c.heads;
     split = blockIdx.y;
@@ -572,7 +576,7 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 // Heads with more rows than a set of columns holds (4 of 128 channels) take more
 // workgroups, which read the same codes again, mostly from cache; two sets in one
 // workgroup need 256 registers and gain nothing (16 sequences of 4000 keys, 32/4 heads,
-// 4 bits: 23.0 us a set each, 23.6 two; 8 bits 31.3 and 43.0).
+// 4 bits: 21.8 us a set each, 23.6 two; 8 bits 29.1 and 43.0).
 // The tile being worked on and its successor, which arrives meanwhile, are both in
 // registers.  512 workgroups of 4 wavefronts: 32 sequences of 8190 keys, 32/8 heads of
 // 128, 4 bits, 68.9 us (4.4 TB/s; a large copy reaches 4.8); 4 of 8000 keys, 32 heads, 8
