@@ -558,38 +558,42 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 
 // Workgroup = one row block of a key head and one chunk of the keys, its 4 wavefronts
 // taking tiles of 32 keys in turn; no LDS and no barrier before the end.  Codes become
-// fp16 operands of v_mfma_f32_16x16x32 by bit operations alone: code bits in the
-// low bits of an fp16 are the subnormal code * 2^-24 (bits 4-7: 16 code * 2^-24), which
-// the instruction multiplies exactly.  Columns n of a product = (query row n / NG, channel group n % NG), NG = HD / 32:
-//  S[key][n]: A = K codes, lane (key row m, lane / 16 = g) holding HD / 4 consecutive
-//    channels, which lie in one group; B = the query, zero outside the column's group; the
-//    codes' offset 2^(BITS - 1) is taken off the sums' start.  So
-//    a lane has the sums of its group for 8 keys, multiplies by the group's K scales and
-//    adds the NG lanes of its row.  Rows 4 g + r of product u are keys 8 g + 4 u + r.
-//  O[ch][n] += V codes * w, the codes' offset taken off them first (a packed fp16 addition,
-//    exact; taken off the sums it would leave errors of an offset times w), w = exp2(score - m) * V scale of the column's group, rounded to
-//    fp16 after division by a power of two kept within 8 of the scales met and times 16 (at
-//    most 2^15: what is rounded below the smallest normal is 2^-26 of the largest).  The 8 keys whose
-//    scores a lane holds are the 8 k slots of its B operand, so w needs no exchange; A row m
-//    of product i is channel (HD / 16) m + i, a lane reading HD / 16 channels of 8 keys.
-//    A lane's own column counts where the channel's group is the column's.
+// fp16 operands of v_mfma_f32_16x16x32 by bit operations alone: code bits in the low
+// bits of an fp16 are the subnormal code * 2^-24 (in bits 4-7: 16 code * 2^-24), which
+// the instruction multiplies exactly.  Columns n of a product are (query row n / NG,
+// channel group n % NG), NG = HD / 32:
+//  S[key][n]: A = K codes, a lane (key row m, lane / 16 = g) holding HD / 4 consecutive
+//    channels, which lie in one group; B = the query, zero outside the column's group;
+//    the codes' offset 2^(BITS - 1) is taken off the sums' start.  So a lane has the sums
+//    of its group for 8 keys, multiplies by the group's K scales and adds the NG lanes of
+//    its row.  Rows 4 g + r of product u are keys 8 g + 4 u + r.
+//  O[ch][n] += V codes * w, the codes' offset taken off them first (a packed fp16
+//    addition, exact; taken off the sums it would leave errors of an offset times w).
+//    w = exp2(score - m) * V scale of the column's group, rounded to fp16 after division
+//    by a power of two kept within 8 of the scales met, and times 16 (at most 2^15, so
+//    that what falls below fp16's smallest normal is 2^-18 of the largest weight or
+//    less).  The 8 keys whose scores a lane holds are the 8 k slots of its B operand: w
+//    needs no exchange.  A row m of product i is channel (HD / 16) m + i, a lane reading
+//    HD / 16 channels of 8 keys.  A lane's own column counts where the channel's group is
+//    the column's.
+// The query is divided by a power of two as well (largest element to 2^14), so that bf16
+// and fp16 rows become fp16 without loss.  The maximum m moves lazily (by more than 2^8).
+// The tile being worked on and its successor, which arrives meanwhile, are both in
+// registers.
 // Heads with more rows than a set of columns holds (4 of 128 channels) take more
 // workgroups, which read the same codes again, mostly from cache; two sets in one
 // workgroup need 256 registers and gain nothing (16 sequences of 4000 keys, 32/4 heads,
 // 4 bits: 21.8 us a set each, 23.6 two; 8 bits 29.1 and 43.0).
-// The tile being worked on and its successor, which arrives meanwhile, are both in
-// registers.  512 workgroups of 4 wavefronts: 32 sequences of 8190 keys, 32/8 heads of
-// 128, 4 bits, 68.9 us (4.4 TB/s; a large copy reaches 4.8); 4 of 8000 keys, 32 heads, 8
-// bits, 59 us (4.7 TB/s).
-// The query is divided by a power of two as well (largest element to 2^14), so that bf16
-// and fp16 rows become fp16 without loss.  The maximum m moves lazily (by more than 2^8).
+// Measured: 32 sequences of 8190 keys, 32/8 heads of 128, 4 bits, 71 us (4.2 TB/s; a large
+// copy reaches 4.8; 250 vector instructions per tile); 4 of 8000 keys, 32 heads, 8 bits,
+// 59 us (4.7 TB/s).
+
 // Wavefronts per SIMD that the registers of a tile, its successor and O leave room for.
 constexpr int cached_waves(int hd, int bits) { return hd == 128 ? (bits == 4 ? 3 : 2) : hd == 64 ? 3 : 4; }
 
 template <typename T, int HD, int BITS, bool CAP>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(cached_waves(HD, BITS), cached_waves(HD, BITS))))
-void k_cached_mfma(gm_cached_attention a, gm_kv_cache c,
-                                                     CachedPlan plan) {
+void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
   constexpr int OFF = 1 << (BITS - 1), NWV = 4, KB = 32;
   constexpr int NG = HD / kKvGroup, RB = 16 / NG;   // groups, rows per block
   constexpr int KD = HD * BITS / 128;               // words of a lane's K chunk
