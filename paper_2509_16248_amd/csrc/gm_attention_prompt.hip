@@ -277,15 +277,21 @@ constexpr int kTiles = 2048;      // key tiles a workgroup keeps marks for (1310
 // Measured, 32 heads of 128, bf16, causal: 2048 tokens 57.7 us (596 TFLOP/s), capped 67.2,
 // biased 65.1, both 77.5; without the causal mask 78.3 (878 TFLOP/s) and 94.0; 8192 tokens
 // and 8 key heads 569 us (966 TFLOP/s), in 7 equal documents 176 (445: tiles that straddle two
-// documents, and workgroups of unequal length).  The matrix cores bound the long plain
-// rows; a capped score costs three transcendental instructions at a quarter rate, 12
-// slots of the 30 per score that the vector units spend against 16 of the matrix cores.
+// documents, and workgroups of unequal length).  What bounds
+// a short row is a tile's chain of dependent steps (1.8 us of 2 workgroups a CU where
+// the matrix cores work 0.9) and that its heaviest workgroup has twice the average;
+// vector instructions taken out of the cap (a polynomial) changed nothing.
 // A hidden key has probability 0, but 0 times an Inf or NaN value is NaN in the
 // matrix product.  Such a product is never finite, so queries whose sums came out
 // not finite are computed again by prompt_row, which skips hidden keys; the loop
 // itself checks nothing.
+
+// Wavefronts per SIMD: as many as the registers leave room for (two at every head size:
+// 4x2048x32 heads of 64, causal, 116 us; three 98).
+constexpr int prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 : 4; }
+
 template <typename T, int HD, bool CAP, bool BIAS, bool FIXED, bool SPARSE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prompt_waves(HD), prompt_waves(HD))))
 void k_prompt_flash(gm_prompt_attention a) {
   constexpr int QB = 128, KB = 64, NW = 4;
   typedef typename Mfma32A<T>::vec vec;
