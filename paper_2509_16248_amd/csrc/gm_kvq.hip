@@ -329,6 +329,7 @@ struct CachedPlan {
   int rows;         // query rows of a key head: Sq * (n_heads / heads)
   int blocks;       // row blocks of a key head
   int nsplit;       // key chunks per row block
+  int waves;        // wavefronts of a workgroup of the MFMA kernel
 };
 
 // The MFMA kernel takes 16-bit dtypes: 16 columns of a product are shared by query
@@ -345,6 +346,12 @@ struct CachedPlan {
 // fp32 kernel, one row a workgroup, wants 1024 of them (8 sequences of 2000 keys, 32/8
 // heads of 128, at 256 / 512 / 1024 / 2048: 60.6 / 43.2 / 37.6 / 38.7) and half the positions
 // (one, 12 heads of 64, capacity 1024, length 300 7.6 / 7.3, 1000 15.7 / 7.5).
+// One or two chunks of at most 256 row blocks, one a CU: a single chunk of 8 wavefronts
+// in place of 4 each, so no merge (4 / 8 wavefronts: 8 sequences, 12 heads of 64, 8 bits,
+// capacity 1024, length 300 6.4 / 6.0, 1000 10.0 / 8.9; 4, 32 heads of 32, 4 bits, 1500
+// 11.9 / 9.9; 32 of 8190, 32/8 heads of 128, 4 bits, 70.0 / 66.8, of 2000, 8 bits, 35.2 /
+// 30.7); a capacity of 256 gives 8 wavefronts a tile each and stays at 4 (one, 32 heads
+// of 128, 4 bits, length 200 6.3 / 6.6).
 CachedPlan cached_plan(const gm_kv_cache& c, int dtype, int B, int Sq, int n_heads) {
   CachedPlan p;
   p.rows = Sq * (n_heads / c.heads);
@@ -356,6 +363,11 @@ CachedPlan cached_plan(const gm_kv_cache& c, int dtype, int B, int Sq, int n_hea
   const long long most = static_cast<long long>(c.max_seq) * c.head_dim > room ? (c.max_seq + 127) / 128 : 1;
   want = want < most ? want : most;
   p.nsplit = static_cast<int>(want < 64 ? want : 64);
+  p.waves = 4;
+  if (dtype != kF32 && p.nsplit <= 2 && wgs <= 256 && c.max_seq > 256) {
+    p.nsplit = 1;
+    p.waves = 8;
+  }
   return p;
 }
 
@@ -556,7 +568,7 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
   }
 }
 
-// Workgroup = one row block of a key head and one chunk of the keys, its 4 wavefronts
+// Workgroup = one row block of a key head and one chunk of the keys, its 4 or 8 wavefronts
 // taking tiles of 32 keys in turn; no LDS and no barrier before the end.  Codes become
 // fp16 operands of v_mfma_f32_16x16x32 by bit operations alone: code bits in the low
 // bits of an fp16 are the subnormal code * 2^-24 (in bits 4-7: 16 code * 2^-24), which
@@ -584,17 +596,17 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 // workgroups, which read the same codes again, mostly from cache; two sets in one
 // workgroup need 256 registers and gain nothing (16 sequences of 4000 keys, 32/4 heads,
 // 4 bits: 21.8 us a set each, 23.6 two; 8 bits 29.1 and 43.0).
-// Measured: 32 sequences of 8190 keys, 32/8 heads of 128, 4 bits, 71 us (4.2 TB/s; a large
+// Measured: 32 sequences of 8190 keys, 32/8 heads of 128, 4 bits, 67 us (4.5 TB/s; a large
 // copy reaches 4.8; 250 vector instructions per tile); 4 of 8000 keys, 32 heads, 8 bits,
 // 59 us (4.7 TB/s).
 
 // Wavefronts per SIMD that the registers of a tile, its successor and O leave room for.
 constexpr int cached_waves(int hd, int bits) { return hd == 128 ? (bits == 4 ? 3 : 2) : hd == 64 ? 3 : 4; }
 
-template <typename T, int HD, int BITS, bool CAP>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(cached_waves(HD, BITS), cached_waves(HD, BITS))))
+template <typename T, int HD, int BITS, bool CAP, int NWV>
+__global__ __launch_bounds__(64 * NWV) __attribute__((amdgpu_waves_per_eu(cached_waves(HD, BITS), cached_waves(HD, BITS))))
 void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
-  constexpr int OFF = 1 << (BITS - 1), NWV = 4, KB = 32;
+  constexpr int OFF = 1 << (BITS - 1), KB = 32;
   constexpr int NG = HD / kKvGroup, RB = 16 / NG;   // groups, rows per block
   constexpr int KD = HD * BITS / 128;               // words of a lane's K chunk
   constexpr int VB = HD * BITS / 128, VD = VB < 4 ? 1 : VB / 4;   // bytes, words of its V chunk
@@ -847,7 +859,7 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
     s_l[wave][n / NG] = l;
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < RB * HD; e += 256) {
+  for (int e = threadIdx.x; e < RB * HD; e += 64 * NWV) {
     const int ch = e % HD, row = e / HD, gr = w.blk * RB + row;
     if (gr >= plan.rows) break;
     float M = -INFINITY, L = 0.f, O = 0.f;
@@ -946,10 +958,19 @@ void launch_attention_cached(const gm_cached_attention& a, hipStream_t s) {
     constexpr int HD = decltype(hd)::value, BITS = decltype(bits)::value;
     if constexpr (std::is_same<T, float>::value)
       hipLaunchKernelGGL((k_cached_rows<T, HD, BITS>), grid, block, 0, s, a, c, p);
-    else if (a.scores.softcap > 0.f)
-      hipLaunchKernelGGL((k_cached_mfma<T, HD, BITS, true>), grid, block, 0, s, a, c, p);
-    else
-      hipLaunchKernelGGL((k_cached_mfma<T, HD, BITS, false>), grid, block, 0, s, a, c, p);
+    else {
+      auto go = [&](auto cap, auto waves) {
+        constexpr int NWV = decltype(waves)::value;
+        hipLaunchKernelGGL((k_cached_mfma<T, HD, BITS, decltype(cap)::value, NWV>), grid, dim3(64 * NWV), 0, s,
+                           a, c, p);
+      };
+      auto width = [&](auto cap) {
+        if (p.waves == 8) go(cap, std::integral_constant<int, 8>());
+        else go(cap, std::integral_constant<int, 4>());
+      };
+      if (a.scores.softcap > 0.f) width(std::true_type());
+      else width(std::false_type());
+    }
     if (p.nsplit > 1)
       hipLaunchKernelGGL((k_cached_merge<T, HD>), dim3(heads * p.rows), block, 0, s, a, c, p);
   });

@@ -67,6 +67,22 @@ def test_cached_long_sequences_are_split(bits, dtype, hd):
     cached_case(dtype, bits, hd, 2, 1, 2, 1, 3000, [3000, 1411], cap=9000)
 
 
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("bits,dtype", [(8, "bf16"), (4, "f16"), (4, "bf16"), (8, "f16")])
+def test_cached_one_chunk_of_eight_wavefronts(bits, dtype, hd):
+    # a capacity over 256 that one chunk holds; lengths that leave wavefronts without a
+    # tile, end inside one and fill two rounds
+    cached_case(dtype, bits, hd, 5, 3, 6, 2, 500, [500, 257, 33, 1, 0], cap=510, softcap=4.0)
+    cached_case(dtype, bits, hd, 2, 1, 2, 2, 290, [289, 255], cap=290, alibi=True)
+
+
+@pytest.mark.parametrize("heads", [4, 5])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_cached_row_blocks_on_either_side_of_one_a_cu(bits, heads):
+    # 64 sequences of 4 key heads are 256 row blocks (one chunk), of 5 are 320 (two)
+    cached_case("bf16", bits, 128, 64, 1, 2 * heads, heads, 700, [700 - 11 * b for b in range(64)])
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_cached_hidden_positions(bits, dtype):
