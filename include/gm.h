@@ -454,7 +454,8 @@ int gm_flush_effects(gm_model *m, gm_effect_cb cb, void *user, int32_t *n_droppe
  * element (b, t, h, c) is at p[b * batch + t * token + h * head + c], strides
  * in elements.  p and the strides of dimensions longer than one must be
  * multiples of 16 bytes; strides may not be negative.  An output's elements may
- * not overlap one another or an input. */
+ * not overlap one another, another tensor or an input (refused where both start
+ * at the same address). */
 typedef struct gm_tensor {
   void* p;
   int64_t batch, token, head;

@@ -122,6 +122,7 @@ int gm_kv_read(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n, co
                const int32_t* count, gm_tensor k, gm_tensor v, hipStream_t stream) {
   if (int rc = check_rows(cache, dtype, B, n, k, v, start, count, nullptr, true)) return rc;
   if (B == 0 || n == 0) return GM_OK;
+  if (k.p == v.p) return inval("k and v overlap");
   launch_kv_read(*cache, dtype, B, n, start, count, k, v, stream);
   return launched();
 }
@@ -153,6 +154,7 @@ int gm_attention_cached(const gm_cached_attention* a, hipStream_t stream) {
   const uint64_t need = attention_cached_workspace(*c, a->dtype, a->B, a->Sq, a->n_heads);
   if (need && (!a->workspace || misaligned(a->workspace, 16) || a->workspace_bytes < need))
     return inval("workspace is NULL, misaligned or smaller than gm_attention_cached_workspace");
+  if (a->out.p == a->q.p) return inval("out and q overlap");
   launch_attention_cached(*a, stream);
   return launched();
 }
@@ -181,6 +183,8 @@ int gm_attention(const gm_prompt_attention* a, hipStream_t stream) {
   // a launch has fewer than 2^32 threads, 256 for 32 query rows of a head
   if (static_cast<double>(a->B) * a->n_heads * ((a->Sq + 31) / 32) >= 16777216.0)
     return inval("B * n_heads * ceil(Sq / 32) must be below 2^24");
+  if (a->out.p == a->q.p || (a->Sk > 0 && (a->out.p == a->k.p || a->out.p == a->v.p)))
+    return inval("out and an input overlap");
   launch_attention_prompt(*a, stream);
   return launched();
 }

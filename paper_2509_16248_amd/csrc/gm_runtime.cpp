@@ -1262,7 +1262,7 @@ int gm_model_create_ex(const gm_config* cfg, const gm_weights* w, const gm_attn_
     if (e == hipSuccess) e = hipMemset(m->seqlen, 0, c.max_batch * sizeof(int32_t));
     if (e == hipSuccess) e = hipMemset(m->dpos, 0, c.max_batch * sizeof(int32_t));
     if (e != hipSuccess) return fail(hip_fail(e, "hipMemset"));
-      if (opt.kv_bits) {
+    if (opt.kv_bits) {
       m->kv_bits = opt.kv_bits;
       const size_t codes = static_cast<size_t>(c.max_batch) * kv_rows * d * opt.kv_bits / 8;
       const size_t scales = static_cast<size_t>(c.max_batch) * kv_rows * (d / kKvGroup) * 2;

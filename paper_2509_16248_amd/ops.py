@@ -9,7 +9,8 @@ float16 on one HIP device.  The channels of a head are contiguous; the base
 address and the other strides are multiples of 16 bytes (views of a fused
 q | k | v projection will do).  Work runs on ``stream`` (default: the current
 stream of the tensors' device), and what a call allocates belongs to it;
-tensors made on another stream have to be ready there.
+tensors made on another stream have to be ready there.  ``out`` may not overlap
+an input.  Forward only: results carry no gradient.
 """
 from __future__ import annotations
 

@@ -135,6 +135,14 @@ def test_prompt_attention_refusals(kw, message):
     refused(lambda: gm.gm_attention(prompt(**kw), 0), message)
 
 
+def test_outputs_may_not_start_where_another_tensor_does():
+    refused(lambda: gm.gm_kv_read(cache(), 1, 2, 8, None, None, tensor(), tensor(), 0), "overlap")
+    refused(lambda: gm.gm_attention_cached(cached(), 0), "overlap")
+    far = dict(q=tensor(p=P + 4096), k=tensor(p=P + 8192), v=tensor(p=P + 16384))
+    for name in far:
+        refused(lambda: gm.gm_attention(prompt(**{**far, name: tensor()}), 0), "overlap")
+
+
 def test_null_arguments():
     L = gm.lib()
     assert L.gm_attention(None, None) == gm.GM_E_INVAL
