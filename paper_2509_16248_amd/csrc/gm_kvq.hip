@@ -776,8 +776,8 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
       most = fmaxf(most, __shfl_xor(most, 16, 64));
       most = fmaxf(most, __shfl_xor(most, 32, 64));
       const uint32_t e = __float_as_uint(most) >> 23;
-      // 2^(e + 1 - 127), its reciprocal a normal number
-      float b = __uint_as_float((e < 2 ? 2 : e > 252 ? 253 : e + 1) << 23);
+      // 2^(e + 1 - 127), its reciprocal a normal number and 16 times that finite
+      float b = __uint_as_float((e < 3 ? 4 : e > 252 ? 253 : e + 1) << 23);
       b = most > 8.f * bound ? b : bound;
       const float ib = __uint_as_float((254u << 23) - __float_as_uint(b));
       const float f = bound > 0.f ? bound * ib : 0.f;

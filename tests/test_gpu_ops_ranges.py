@@ -1,0 +1,48 @@
+"""The attention and KV-cache operators at the ends of the ranges they accept,
+against the definitions in float64 (tolerances: ops_reference.attention)."""
+import pytest
+import torch
+
+import ops_reference as ref
+from paper_2509_16248_amd import ops
+from paper_2509_16248_amd.ops import KvCache
+
+pytestmark = pytest.mark.gpu
+
+
+def rows(shape, dtype, seed, size=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * size).to(ref.DT[dtype])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("exponent", [-119, -123, -127, -131])
+def test_cached_values_of_the_smallest_scales(bits, hd, exponent):
+    """Value scales down to the smallest subnormals: alone, next to groups of zeros,
+    next to hidden positions, and before tiles of ordinary values.
+
+    A weight is p s 16 / b in fp16, b a power of two that is at most twice the largest
+    scale met or, for scales as small as these, 2^-123.  Half a step of fp16's subnormals,
+    2^-25, then stands for 2^-25 2^-123 / 16 = 2^-152, times a code of at most 2^7 for each
+    of n keys: n 2^-145 on top of the tolerance."""
+    B, n, H = 1, 600, 2
+    q, k = rows((B, 1, H, hd), "bf16", 1), rows((B, n, H, hd), "bf16", 2)
+    tiny = rows((B, n, H, hd), "f32", 3) * 2.0 ** exponent
+    zeros, later = tiny.clone(), tiny.clone()
+    zeros[:, 1::3] = 0
+    later[:, 256:] *= 2.0 ** (-exponent)          # every wavefront's first tile is tiny
+    mask = torch.ones(B, n, dtype=torch.int32)
+    mask[:, 2::5] = 0
+    for what, v, m in (("alone", tiny, None), ("zeros", zeros, None), ("hidden", tiny, mask),
+                       ("later", later, None), ("later, hidden", later, mask)):
+        v = v.to(torch.bfloat16)
+        for cap in (n, 40000):                    # one chunk, and several with a merge
+            c = KvCache(B, H, cap, hd, bits=bits, masked=m is not None)
+            c.write(k.cuda(), v.cuda(), mask=None if m is None else m.cuda())
+            for length in (n, 100):
+                got = ops.cached_attention(q.cuda(), c, torch.tensor([length], dtype=torch.int32).cuda())
+                tol = torch.zeros(q.shape, dtype=torch.float64)
+                want = ref.cached(q, k, v, [length], bits, valid=m, tol=tol)
+                tol += n * 2.0 ** -145
+                ref.check(got, want, tol, f"2^{exponent} q{bits} hd{hd} {what} cap {cap} length {length}")
