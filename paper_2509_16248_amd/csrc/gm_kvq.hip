@@ -250,8 +250,9 @@ __global__ __launch_bounds__(256) void k_kv_read(KvRows a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t code = BITS == 8 ? (w[u][j / 4] >> (8 * (j % 4))) & 255u : (w[u][0] >> (4 * j)) & 15u;
-      // (code - OFF) s, which fp32 holds exactly; rows that are not there have s = 0
-      row.set(j, fmaf(static_cast<float>(code), s, -OFF * s));
+      // (code - OFF) s, exact in fp32 up to its largest number (which OFF s by itself may
+      // pass); rows that are not there have s = 0 and become +0
+      row.set(j, fmaf(static_cast<float>(code) - OFF, s, 0.f));
     }
     row.store(kv_row<T>(a, place[u]));
   }

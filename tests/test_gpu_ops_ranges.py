@@ -46,3 +46,24 @@ def test_cached_values_of_the_smallest_scales(bits, hd, exponent):
                 want = ref.cached(q, k, v, [length], bits, valid=m, tol=tol)
                 tol += n * 2.0 ** -145
                 ref.check(got, want, tol, f"2^{exponent} q{bits} hd{hd} {what} cap {cap} length {length}")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_finite_groups_up_to_the_largest_number_read_back(bits, dtype):
+    """Groups whose largest element is near the end of the type's range, with zeros and
+    both signs: every stored value is code * scale, Inf only where that product is."""
+    tops = [2.9e38, 3.0e38, 3.2e38, 3.38e38, 3.3895e38]
+    x = torch.linspace(-1, 1, 32, dtype=torch.float64).repeat(len(tops), 1)
+    x *= torch.tensor(tops, dtype=torch.float64)[:, None]
+    x[:, 5], x[:, 9], x[:, 20] = 0, 1e30, -1e36
+    x = x.to(ref.DT[dtype])[None, :, None]
+    assert torch.isfinite(x).all()
+    c = KvCache(1, 1, 64, 32, bits=bits)
+    c.write(x.cuda(), (-x).cuda())
+    k, v = c.read(len(tops), dtype=ref.DT[dtype])
+    want = ref.stored(x, bits).to(ref.DT[dtype])
+    # (Q * scale may round to Inf, scale having been rounded up; no smaller code's value does)
+    smaller = ref.quantise(x, bits)[0].abs() < (127 if bits == 8 else 7)
+    assert smaller.any() and torch.isfinite(want[smaller]).all()
+    assert torch.equal(k.cpu(), want) and torch.equal(v.cpu(), -want)
