@@ -516,8 +516,9 @@ typedef struct gm_scores {
  * h / (n_heads / cache->heads).  Softmax statistics and sums are fp32; for
  * 16-bit dtypes a probability times a value's scale is rounded to fp16.
  * workspace: device, 16-byte aligned, at least
- * gm_attention_cached_workspace(...) bytes (which may be 0: then NULL will do),
- * used by this call alone until it has run. */
+ * gm_attention_cached_workspace(...) bytes (which may be 0: then NULL will do;
+ * 0 too for sizes that the call refuses), used by this call alone until it has
+ * run. */
 typedef struct gm_cached_attention {
   const gm_kv_cache* cache;
   int32_t dtype, B, Sq, n_heads;

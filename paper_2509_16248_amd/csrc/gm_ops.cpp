@@ -99,6 +99,11 @@ int check_scores(const gm_scores& s) {
   return GM_OK;
 }
 
+// The query rows of a call fit one launch.
+bool cached_fits(int B, int Sq, int n_heads) {
+  return static_cast<double>(B) * Sq * n_heads < 16777216.0;
+}
+
 int launched() {
   HIP_TRY(hipGetLastError());
   return GM_OK;
@@ -129,8 +134,8 @@ int gm_kv_read(const gm_kv_cache* cache, int32_t dtype, int32_t B, int32_t n, co
 
 uint64_t gm_attention_cached_workspace(const gm_kv_cache* cache, int32_t dtype, int32_t B,
                                        int32_t Sq, int32_t n_heads) {
-  if (check_cache(cache) || check_dtype(dtype) || B < 1 || Sq < 1 || n_heads < 1 ||
-      n_heads % cache->heads)
+  if (check_cache(cache) || check_dtype(dtype) || B < 1 || B > cache->batch || Sq < 1 ||
+      Sq > cache->max_seq || n_heads < 1 || n_heads % cache->heads || !cached_fits(B, Sq, n_heads))
     return 0;
   return attention_cached_workspace(*cache, dtype, B, Sq, n_heads);
 }
@@ -149,8 +154,7 @@ int gm_attention_cached(const gm_cached_attention* a, hipStream_t stream) {
     return rc;
   if (a->B == 0 || a->Sq == 0) return GM_OK;
   if (!a->lengths || misaligned(a->lengths, 4)) return inval("lengths must be a 4-byte aligned pointer");
-  if (static_cast<double>(a->B) * a->Sq * a->n_heads >= 16777216.0)
-    return inval("B * Sq * n_heads must be below 2^24");
+  if (!cached_fits(a->B, a->Sq, a->n_heads)) return inval("B * Sq * n_heads must be below 2^24");
   const uint64_t need = attention_cached_workspace(*c, a->dtype, a->B, a->Sq, a->n_heads);
   if (need && (!a->workspace || misaligned(a->workspace, 16) || a->workspace_bytes < need))
     return inval("workspace is NULL, misaligned or smaller than gm_attention_cached_workspace");
