@@ -201,13 +201,15 @@ class GmModel:
 
     def read_cache(self, layer: int, n: int, batch: Optional[int] = None, stream=None):
         """k and v [B, n, n_heads, head_dim] of positions 0 .. n - 1 as the
-        quantised cache of a layer holds them (gm_kv_read; ``kv_bits`` models)."""
+        quantised cache of a layer holds them (gm_kv_read; ``kv_bits`` models).
+        They belong to ``stream`` (default: the current one), which reads them."""
         c = gm.gm_model_kv_cache(self.handle, layer)
         B = c.batch if batch is None else batch
         shape = (B, n, c.heads, c.head_dim)
-        k, v = (torch.empty(shape, dtype=_TORCH[self.cfg.dtype], device=self.device) for _ in "kv")
-        kt, vt = (gm.gm_tensor(t.data_ptr(), *t.stride()[:3]) for t in (k, v))
-        with torch.cuda.device(self.device):
+        with torch.cuda.device(self.device), torch.cuda.stream(stream):
+            # (memory of another stream might still be in use there)
+            k, v = (torch.empty(shape, dtype=_TORCH[self.cfg.dtype], device=self.device) for _ in "kv")
+            kt, vt = (gm.gm_tensor(t.data_ptr(), *t.stride()[:3]) for t in (k, v))
             gm.gm_kv_read(c, _DTYPES[self.cfg.dtype], B, n, None, None, kt, vt, self._stream(stream))
         return k, v
 
