@@ -260,8 +260,10 @@ constexpr int kTiles = 2048;      // key tiles a workgroup keeps marks for (1310
 // What the scores go through instead:
 //  CAP   softcap tanh(x / softcap) = C - 2 C / (exp2(x c2) + 1) in log2 units, C =
 //        softcap log2(e): two transcendental and three other instructions
-//  BIAS  a subtraction and a multiplication make the distance's share, from which the
-//        products' sums start (after a cap: a subtraction and an fma)
+//  BIAS  a subtraction, a multiplication and an fma (after a cap: a subtraction and an
+//        fma).  It is added after the scale: slope / scale, from which the products' sums
+//        could start, overflows under tiny scales, and what is added to far distances in
+//        units of q.k is rounded at every step of the sums.
 //  masks a 64-bit word per lane and tile: key mask (a ballot of wavefront 0), causal
 //        and prefix bounds (shifts) and documents (32 comparisons where the tile or
 //        the wavefront's queries hold more than one); none at all for a tile that is
@@ -355,9 +357,8 @@ void k_prompt_flash(gm_prompt_attention a) {
   }
   const float c2 = CAP ? a.scores.scale * (2.f * kLog2e) / a.scores.softcap : a.scores.scale * kLog2e;
   const float capc = a.scores.softcap * kLog2e;
-  // the slope, negative, in the units of the scores it is added to: log2 units after a
-  // cap, q.k before the scale without one
-  const float slope1 = BIAS ? a.scores.slopes[h] * (CAP ? -kLog2e : -1.f / a.scores.scale) : 0.f;
+  const float slope2 = BIAS ? a.scores.slopes[h] * -kLog2e : 0.f;
+  constexpr bool LOG2 = CAP || BIAS;          // scores are in log2 units before their maximum is taken
 
   const int qd = kd ? a.q_doc[static_cast<long long>(b) * Sq + (qi < Sq ? qi : Sq - 1)] : 0;
   if constexpr (SPARSE) {
@@ -507,12 +508,10 @@ void k_prompt_flash(gm_prompt_attention a) {
     }
     // ---- S^T = K Q^T: two 32-key blocks
     f32x16 sacc[2];
-    const float dist = static_cast<float>(qpos - kb - 4 * h2);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        sacc[kk][i] = BIAS && !CAP ? slope1 * fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))) : 0.f;
+      for (int i = 0; i < 16; ++i) sacc[kk][i] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
@@ -531,12 +530,14 @@ void k_prompt_flash(gm_prompt_attention a) {
           sacc[kk][i] = fmaf(-2.f * capc, __builtin_amdgcn_rcpf(e), capc);
         }
     }
-    if constexpr (CAP && BIAS) {
+    if constexpr (BIAS) {
+      const float dist = static_cast<float>(qpos - kb - 4 * h2);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          sacc[kk][i] = fmaf(slope1, fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))), sacc[kk][i]);
+          sacc[kk][i] = fmaf(slope2, fabsf(dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3))),
+                             CAP ? sacc[kk][i] : sacc[kk][i] * c2);
     }
     // ---- masks
     const int last = qw0 + off > pre - 1 ? qw0 + off : pre - 1;
@@ -571,7 +572,7 @@ void k_prompt_flash(gm_prompt_attention a) {
       for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
-      float mt = CAP ? mx : mx * c2;
+      float mt = LOG2 ? mx : mx * c2;
       if (__ballot(mt > mrun + kTau)) {        // move the maximum (wavefront-uniform)
         mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
         const float mnew = fmaxf(mrun, mt);
@@ -593,8 +594,8 @@ void k_prompt_flash(gm_prompt_attention a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float s0 = sacc[kk][8 * hf + 2 * j], s1 = sacc[kk][8 * hf + 2 * j + 1];
-          const float p0 = __builtin_amdgcn_exp2f(FIXED ? s0 : CAP ? s0 - msub : fmaf(s0, c2, -msub));
-          const float p1 = __builtin_amdgcn_exp2f(FIXED ? s1 : CAP ? s1 - msub : fmaf(s1, c2, -msub));
+          const float p0 = __builtin_amdgcn_exp2f(FIXED ? s0 : LOG2 ? s0 - msub : fmaf(s0, c2, -msub));
+          const float p1 = __builtin_amdgcn_exp2f(FIXED ? s1 : LOG2 ? s1 - msub : fmaf(s1, c2, -msub));
           lrun += p0 + p1;
           w[j] = pack2<T>(p0, p1);
         }

@@ -67,3 +67,22 @@ def test_finite_groups_up_to_the_largest_number_read_back(bits, dtype):
     smaller = ref.quantise(x, bits)[0].abs() < (127 if bits == 8 else 7)
     assert smaller.any() and torch.isfinite(want[smaller]).all()
     assert torch.equal(k.cpu(), want) and torch.equal(v.cpu(), -want)
+
+
+@pytest.mark.parametrize("softcap", [0.0, 30.0])
+@pytest.mark.parametrize("dtype,scale", [("bf16", 1e-37), ("f16", 1e-37), ("f32", 1e-37), ("bf16", 1e-30),
+                                         ("f16", 1e-3), ("bf16", 1e30), ("f32", 1e30)])
+def test_prompt_biases_under_any_scale(dtype, softcap, scale):
+    """A distance bias next to products that a tiny scale makes vanish (or a large one
+    lets dominate), where only far keys are visible."""
+    B, S, H, hd = 1, 150, 2, 64
+    size = 1e-16 if scale > 1 else 1.0            # scores of a size that a softmax tells apart
+    q, k, v = rows((B, S, H, hd), dtype, 1, size), rows((B, S, H, hd), dtype, 2, size), rows((B, S, H, hd), dtype, 3)
+    slopes = torch.tensor([1.0, 0.25])
+    mask = (torch.arange(S) < 8).int()[None]
+    kw = dict(causal=True, softcap=softcap, scale=scale)
+    got = ops.attention(q.cuda(), k.cuda(), v.cuda(), slopes=slopes.cuda(), key_mask=mask.cuda(), **kw)
+    tol = torch.zeros(q.shape, dtype=torch.float64)
+    want = ref.prompt(q, k, v, slopes=slopes, key_mask=mask, tol=tol, **kw)
+    assert want.abs().amax(-1).gt(0).all()
+    ref.check(got, want, tol, f"{dtype} cap {softcap} scale {scale:g}")
