@@ -247,10 +247,6 @@ void prompt_f32(const gm_prompt_attention& a, hipStream_t s) {
 // 32 bits of four consecutive int32, at any 4-byte address.
 typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));
 
-// Caps up to which bf16 scores need no running maximum: exp2(score) and its sums stay
-// within 2^72 2^24 times the values, far from the ends of bf16 and fp32.
-constexpr float kFixedCap = 50.f;
-
 constexpr int kTiles = 2048;      // key tiles a workgroup keeps marks for (131072 keys)
 
 // Workgroup = 128 queries of one (sequence, head), as k_flash (gm_attention.hip)
@@ -292,7 +288,7 @@ constexpr int kTiles = 2048;      // key tiles a workgroup keeps marks for (1310
 // 4x2048x32 heads of 64, causal, 116 us; three 98).
 constexpr int prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 : 4; }
 
-template <typename T, int HD, bool CAP, bool BIAS, bool FIXED, bool SPARSE>
+template <typename T, int HD, bool CAP, bool BIAS, bool SPARSE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(prompt_waves(HD), prompt_waves(HD))))
 void k_prompt_flash(gm_prompt_attention a) {
   constexpr int QB = 128, KB = 64, NW = 4;
@@ -565,25 +561,22 @@ void k_prompt_flash(gm_prompt_attention a) {
     }
     // fp16 probabilities times 2^7 (at most 2^15): fewer fall below its smallest normal
     constexpr float kUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
-    float msub = 0.f;
-    if constexpr (!FIXED) {
-      float mx = -INFINITY;
+    float mx = -INFINITY;
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk)
+    for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
-      float mt = LOG2 ? mx : mx * c2;
-      if (__ballot(mt > mrun + kTau)) {        // move the maximum (wavefront-uniform)
-        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-        const float mnew = fmaxf(mrun, mt);
-        const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
-        lrun *= alpha;
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
+    float mt = LOG2 ? mx : mx * c2;
+    if (__ballot(mt > mrun + kTau)) {          // move the maximum (wavefront-uniform)
+      mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+      const float mnew = fmaxf(mrun, mt);
+      const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+      lrun *= alpha;
 #pragma unroll
-        for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
-        mrun = mnew;
-      }
-      msub = mrun == -INFINITY ? 0.f : mrun - kUp;
+      for (int c = 0; c < CB; ++c) oacc[c] *= alpha;
+      mrun = mnew;
     }
+    const float msub = mrun == -INFINITY ? 0.f : mrun - kUp;
     // ---- probabilities, their sum, and P^T as 16-bit B operands
     vec pb[4];
 #pragma unroll
@@ -594,8 +587,8 @@ void k_prompt_flash(gm_prompt_attention a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float s0 = sacc[kk][8 * hf + 2 * j], s1 = sacc[kk][8 * hf + 2 * j + 1];
-          const float p0 = __builtin_amdgcn_exp2f(FIXED ? s0 : LOG2 ? s0 - msub : fmaf(s0, c2, -msub));
-          const float p1 = __builtin_amdgcn_exp2f(FIXED ? s1 : LOG2 ? s1 - msub : fmaf(s1, c2, -msub));
+          const float p0 = __builtin_amdgcn_exp2f(LOG2 ? s0 - msub : fmaf(s0, c2, -msub));
+          const float p1 = __builtin_amdgcn_exp2f(LOG2 ? s1 - msub : fmaf(s1, c2, -msub));
           lrun += p0 + p1;
           w[j] = pack2<T>(p0, p1);
         }
@@ -684,21 +677,18 @@ void prompt_flash(const gm_prompt_attention& a, hipStream_t s) {
   const bool cap = a.scores.softcap > 0.f, bias = a.scores.slopes;
   const std::true_type yes;
   const std::false_type no;
-  auto launch = [&](auto c, auto b, auto fixed) {
+  auto launch = [&](auto c, auto b) {
     auto go = [&](auto sparse) {
-      hipLaunchKernelGGL((k_prompt_flash<T, HD, decltype(c)::value, decltype(b)::value,
-                                         decltype(fixed)::value, decltype(sparse)::value>),
+      hipLaunchKernelGGL((k_prompt_flash<T, HD, decltype(c)::value, decltype(b)::value, decltype(sparse)::value>),
                          grid, block, 0, s, a);
     };
     if (a.key_mask || a.q_doc) go(yes);
     else go(no);
   };
-  if constexpr (std::is_same<T, bf16_t>::value)
-    if (cap && !bias && a.scores.softcap <= kFixedCap) return launch(yes, no, yes);
-  if (cap && bias) launch(yes, yes, no);
-  else if (cap) launch(yes, no, no);
-  else if (bias) launch(no, yes, no);
-  else launch(no, no, no);
+  if (cap && bias) launch(yes, yes);
+  else if (cap) launch(yes, no);
+  else if (bias) launch(no, yes);
+  else launch(no, no);
 }
 
 }  // namespace

@@ -86,3 +86,23 @@ def test_prompt_biases_under_any_scale(dtype, softcap, scale):
     want = ref.prompt(q, k, v, slopes=slopes, key_mask=mask, tol=tol, **kw)
     assert want.abs().amax(-1).gt(0).all()
     ref.check(got, want, tol, f"{dtype} cap {softcap} scale {scale:g}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("softcap", [20.0, 50.0, 51.0])
+@pytest.mark.parametrize("side", [-1, 1])
+@pytest.mark.parametrize("exponent", [-100, 0, 100])
+def test_capped_prompts_whose_scores_all_lie_at_one_end(dtype, softcap, side, exponent):
+    """Every visible score near -cap or +cap, with small and large values: a softmax
+    does not depend on what its scores have in common."""
+    B, S, H, hd = 1, 140, 2, 64
+    # scores near 1.2 times the cap before it
+    size = (1.2 * softcap / hd ** 0.5) ** 0.5
+    q = (size + rows((B, S, H, hd), "f32", 1) * 0.05).to(ref.DT[dtype])
+    k = (side * size + rows((B, S, H, hd), "f32", 2) * 0.5).to(ref.DT[dtype])
+    v = rows((B, S, H, hd), dtype, 3, 2.0 ** exponent)
+    for causal in (True, False):
+        got = ops.attention(q.cuda(), k.cuda(), v.cuda(), causal=causal, softcap=softcap)
+        tol = torch.zeros(q.shape, dtype=torch.float64)
+        want = ref.prompt(q, k, v, causal=causal, softcap=softcap, tol=tol)
+        ref.check(got, want, tol, f"{dtype} cap {softcap} side {side} 2^{exponent} causal {causal}")
