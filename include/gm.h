@@ -532,9 +532,11 @@ int gm_attention_cached(const gm_cached_attention* a, hipStream_t stream);
 uint64_t gm_attention_cached_workspace(const gm_kv_cache* cache, int32_t dtype, int32_t B,
                                        int32_t Sq, int32_t n_heads);
 
-/* The cache of one layer of a model with kv_bits, for gm_kv_read (handing a
- * sequence over, inspection) and gm_kv_write (taking one over).  It lives as long
- * as the model; a forward or decode step in flight on another stream races. */
+/* The cache of one layer of a model with kv_bits, for gm_kv_read (inspection,
+ * handing a sequence's rows over).  To be read only: the model keeps its
+ * sequences' lengths itself, a decode step continues what its own last prefill
+ * stored, and the valid bytes are one array for all layers.  It lives as long as
+ * the model; a forward or decode step in flight on another stream races. */
 int gm_model_kv_cache(const gm_model *m, int32_t layer, gm_kv_cache *out);
 
 /* Attention over whole prompts.  Query i of a sequence is at position
