@@ -583,12 +583,13 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 //  O[ch][n] += V codes * w, the codes' offset taken off them first (a packed fp16
 //    addition, exact; taken off the sums it would leave errors of an offset times w).
 //    w = exp2(score - m) * V scale of the column's group, rounded to fp16 after division
-//    by a power of two kept within 8 of the scales met, and times 16 (at most 2^15, so
-//    that what falls below fp16's smallest normal is 2^-18 of the largest weight or
-//    less).  The 8 keys whose scores a lane holds are the 8 k slots of its B operand: w
-//    needs no exchange.  A row m of product i is channel (HD / 16) m + i, a lane reading
-//    HD / 16 channels of 8 keys.  A lane's own column counts where the channel's group is
-//    the column's.
+//    by a power of two above the largest weight at the last look and at least an eighth
+//    of any since, and times 2^12 (at most 2^15, so that what falls below fp16's smallest
+//    normal is 2^-25 of the largest weight or less; in units of the largest scale a value
+//    of no weight would take the bits of all others).  The 8 keys whose scores a lane
+//    holds are the 8 k slots of its B operand: w needs no exchange.  A row m of product i
+//    is channel (HD / 16) m + i, a lane reading HD / 16 channels of 8 keys.  A lane's own
+//    column counts where the channel's group is the column's.
 // The query is divided by a power of two as well (largest element to 2^14), so that bf16
 // and fp16 rows become fp16 without loss.  The maximum m moves lazily (by more than 2^8).
 // The tile being worked on and its successor, which arrives meanwhile, are both in
@@ -695,7 +696,10 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
   };
 
   float m = -INFINITY, l = 0.f;
-  float bound = 0.f, inv_bound = 0.f;               // power of two at or above the V scales met
+  // the largest weight p * V scale at the last look; one over the power of two above it
+  // (2^-115 to 2^126, so that 2^12 times this is finite)
+  float peak = 0.f, inv_unit = __uint_as_float((127u + 115) << 23);
+  auto unit_of = [](float inv) { return __uint_as_float((254u << 23) - __float_as_uint(inv)); };
   f32x4 o[NI];
 #pragma unroll
   for (int e = 0; e < NI; ++e) o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -759,43 +763,40 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
       }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      top = fmaxf(top, s[j]);
-      most = fmaxf(most, sv[j]);
-    }
-    if (__ballot(top > m + kTau)) {
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j]);
+    float f = 1.f;
+    const bool moved = __ballot(top > m + kTau) != 0;
+    if (moved) {
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float mn = fmaxf(m, top);
-      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       l *= f;
-#pragma unroll
-      for (int e = 0; e < NI; ++e) o[e] *= f;
       m = mn;
-    }
-    if (__ballot(most > 8.f * bound)) {
-      most = fmaxf(most, __shfl_xor(most, 16, 64));
-      most = fmaxf(most, __shfl_xor(most, 32, 64));
-      const uint32_t e = __float_as_uint(most) >> 23;
-      // 2^(e + 1 - 127), its reciprocal a normal number and 16 times that finite
-      float b = __uint_as_float((e < 3 ? 4 : e > 252 ? 253 : e + 1) << 23);
-      b = most > 8.f * bound ? b : bound;
-      const float ib = __uint_as_float((254u << 23) - __float_as_uint(b));
-      const float f = bound > 0.f ? bound * ib : 0.f;
-#pragma unroll
-      for (int e2 = 0; e2 < NI; ++e2) o[e2] *= f;
-      bound = b;
-      inv_bound = ib;
     }
     // ---- weights
     const float msub = m == -INFINITY ? 0.f : m;
-    f16x8 wf;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float p = __builtin_amdgcn_exp2f(s[j] - msub);
-      l += p;
-      wf[j] = static_cast<_Float16>(p * (sv[j] * (16.f * inv_bound)));
+      s[j] = __builtin_amdgcn_exp2f(s[j] - msub);
+      l += s[j];
+      most = fmaxf(most, s[j] * sv[j]);
     }
+    // a weight past 8 times that, or a new maximum, under which the old ones count for less
+    if (moved || __ballot(most > 8.f * peak)) {
+      most = fmaxf(most, __shfl_xor(most, 16, 64));
+      most = fmaxf(most, __shfl_xor(most, 32, 64));
+      peak = fminf(fmaxf(peak * f, most), 3.4028234e38f);   // (a product past fp32: its largest)
+      const uint32_t e = __float_as_uint(peak) >> 23;
+      f *= unit_of(inv_unit);                       // (old / new unit alone may pass fp32)
+      inv_unit = __uint_as_float((e < 11 ? 242 : e > 252 ? 1 : 253 - e) << 23);
+      f *= inv_unit;
+#pragma unroll
+      for (int e2 = 0; e2 < NI; ++e2) o[e2] *= f;
+    }
+    f16x8 wf;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) wf[j] = static_cast<_Float16>(s[j] * (sv[j] * (4096.f * inv_unit)));
     // ---- O += V w: word j of product e holds keys 2 j (low half) and 2 j + 1
     if constexpr (BITS == 4) {
 #pragma unroll
@@ -850,9 +851,9 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int x = 0; x < NI; ++x) {
-        const float unit = BITS == 4 && x % 2 ? 65536.f : 1048576.f;   // 2^20 or 2^24, over 16
+        const float unit = BITS == 4 && x % 2 ? 256.f : 4096.f;   // 2^20 or 2^24, over 2^12
         s_o[wave][n / NG][NI * (4 * g + e) + x] =
-            l == 0.f ? 0.f : (o[x][e] * unit * inv) * bound;
+            l == 0.f ? 0.f : (o[x][e] * unit * inv) * unit_of(inv_unit);
       }
   }
   if (t == 0 && g == 0) {

@@ -106,3 +106,39 @@ def test_capped_prompts_whose_scores_all_lie_at_one_end(dtype, softcap, side, ex
         tol = torch.zeros(q.shape, dtype=torch.float64)
         want = ref.prompt(q, k, v, causal=causal, softcap=softcap, tol=tol)
         ref.check(got, want, tol, f"{dtype} cap {softcap} side {side} 2^{exponent} causal {causal}")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype,hd,ratio", [("bf16", 128, 2.0 ** 30), ("bf16", 32, 2.0 ** 60), ("f16", 64, 2.0 ** 22)])
+@pytest.mark.parametrize("at", [0, 45, 301, 599])
+def test_cached_large_values_of_no_weight(bits, dtype, hd, ratio, at):
+    """A key whose values are far larger than the others', and whose weight is nothing:
+    the others' values come out with all of their bits.
+
+    A weight p s is held in fp16 in units of b / 16, b a power of two at most twice the
+    largest weight: half a step of fp16's subnormals, 2^-25, is 2^-28 of that weight, times
+    a code of at most Q, for each of n keys."""
+    B, n, H = 1, 600, 2
+    # scores: 0.8 |q| |k| cos with one key at -90 or so, against a spread of a few units
+    q, k = rows((B, 1, H, hd), "f32", 1).abs() + 0.5, rows((B, n, H, hd), "f32", 2, 0.2)
+    v = rows((B, n, H, hd), "f32", 3)
+    if dtype == "f16":
+        v = v * 2.0 ** -8
+    # exp(-90) 2^60 of an ordinary value is 2^-69 of it
+    k[:, at] = -90 / hd ** 0.5 * (q / (q * q).sum(-1, keepdim=True) * hd)[:, 0]
+    v[:, at] *= ratio
+    q, k, v = (x.to(ref.DT[dtype]) for x in (q, k, v))
+    assert torch.isfinite(v).all()
+    ks, vs = ref.stored(k, bits), ref.stored(v, bits)
+    scores = torch.einsum("hc,nhc->hn", q[0, 0].double(), ks[0]) / hd ** 0.5
+    assert (scores.amax(1) - scores[:, at]).min() > 80
+    for cap in (n, 40000):                            # one chunk, and several with a merge
+        c = KvCache(B, H, cap, hd, bits=bits)
+        c.write(k.cuda(), v.cuda())
+        got = ops.cached_attention(q.cuda(), c, torch.tensor([n], dtype=torch.int32).cuda())
+        tol = torch.zeros((1, H, hd), dtype=torch.float64)
+        want = ref.attention(q[0], ks[0], vs[0], torch.ones(1, n, dtype=torch.bool),
+                             torch.zeros(1, n), hd ** -0.5, tol=tol)
+        others = torch.arange(n) != at
+        tol += n * 2.0 ** -28 * (1 + 2.0 ** -7) * vs[0, others].abs().max()
+        ref.check(got[0], want, tol, f"{dtype} q{bits} hd{hd} at {at} cap {cap}")
