@@ -108,6 +108,44 @@ def test_capped_prompts_whose_scores_all_lie_at_one_end(dtype, softcap, side, ex
         ref.check(got, want, tol, f"{dtype} cap {softcap} side {side} 2^{exponent} causal {causal}")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_operator_on_another_stream_gives_the_same_bits(dtype):
+    B, H, hd, n = 2, 4, 64, 500
+    k, v = rows((B, n, H, hd), dtype, 2).cuda(), rows((B, n, H, hd), dtype, 4).cuda()
+    q = rows((B, n, H, hd), dtype, 3).cuda()
+    lengths = torch.tensor([n, 77], dtype=torch.int32, device="cuda")
+    here, there = (KvCache(B, H, n, hd, bits=8) for _ in range(2))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    there.write(k, v, stream=s)
+    a = [*there.read(n, dtype=ref.DT[dtype], stream=s),
+         ops.cached_attention(q[:, :1], there, lengths, stream=s),
+         ops.attention(q, k, v, causal=True, softcap=30.0, stream=s)]
+    here.write(k, v)
+    b = [*here.read(n, dtype=ref.DT[dtype]), ops.cached_attention(q[:, :1], here, lengths),
+         ops.attention(q, k, v, causal=True, softcap=30.0)]
+    torch.cuda.synchronize()
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype,hd,H,Hkv", [("bf16", 128, 8, 2), ("f16", 64, 4, 4), ("f32", 32, 4, 1)])
+@pytest.mark.parametrize("Sq,lengths", [(64, [300, 64, 70]), (129, [299, 129, 40]), (256, [256, 300, 0])])
+def test_cached_chunks_of_tokens(bits, dtype, hd, H, Hkv, Sq, lengths):
+    """A chunk of a prompt over what is stored, up to the whole cache: lengths equal to
+    the chunk, one more, and short of it."""
+    B, n = 3, 300
+    q = rows((B, Sq, H, hd), dtype, 1)
+    k, v = rows((B, n, Hkv, hd), dtype, 2), rows((B, n, Hkv, hd), dtype, 3)
+    c = KvCache(B, Hkv, n, hd, bits=bits)
+    c.write(k.cuda(), v.cuda())
+    got = ops.cached_attention(q.cuda(), c, torch.tensor(lengths, dtype=torch.int32).cuda(), softcap=20.0)
+    tol = torch.zeros(q.shape, dtype=torch.float64)
+    want = ref.cached(q, k, v, lengths, bits, 20.0, tol=tol)
+    ref.check(got, want, tol, f"{dtype} q{bits} hd{hd} {Sq}x{H}/{Hkv}")
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("dtype,hd,ratio", [("bf16", 128, 2.0 ** 30), ("bf16", 32, 2.0 ** 60), ("f16", 64, 2.0 ** 22)])
 @pytest.mark.parametrize("at", [0, 45, 301, 599])
