@@ -427,12 +427,23 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
   const int qpos = w.len - a.Sq + i;
   const int k1 = w.k1 < qpos + 1 ? w.k1 : qpos + 1;
   const float slope = a.scores.slopes ? a.scores.slopes[h] : 0.f;
-  float q[8];
+  float q[8], scale = a.scores.scale;
   {
     Row8<T> r;
     r.load(static_cast<const T*>(a.q.p) + w.b * a.q.batch + i * a.q.token + h * a.q.head + 8 * gl);
+    float big = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = r.get(j);
+    for (int j = 0; j < 8; ++j) {
+      q[j] = r.get(j);
+      big = fmaxf(big, fabsf(q[j]));
+    }
+    // a row whose sums of products with codes might pass fp32: 2^-32 of it, the same for
+    // all of its lanes
+    if (__builtin_expect(__ballot(big > 0x1p100f) != 0, 0)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] *= 0x1p-32f;
+      scale *= 0x1p32f;
+    }
   }
   const long long head = static_cast<long long>(w.b) * c.heads + w.kvh;
   const char* kc = static_cast<const char*>(c.k) + head * c.max_seq * (HD * BITS / 8) + gl * BITS;
@@ -484,7 +495,7 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
 #pragma unroll
       for (int off = G / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
       if (key >= k1 || !on[u]) continue;       // the same for the whole lane group
-      s = modify_score(s * a.scores.scale, a.scores.softcap, slope, static_cast<float>(qpos - key));
+      s = modify_score(s * scale, a.scores.softcap, slope, static_cast<float>(qpos - key));
       const float mn = fmaxf(m, s), sv = bf16_value(vscale[u]);
       const float corr = m == mn ? 1.f : expf(m - mn), p = s == -INFINITY ? 0.f : expf(s - mn);
       l = l * corr + p;

@@ -180,3 +180,24 @@ def test_cached_large_values_of_no_weight(bits, dtype, hd, ratio, at):
         others = torch.arange(n) != at
         tol += n * 2.0 ** -28 * (1 + 2.0 ** -7) * vs[0, others].abs().max()
         ref.check(got[0], want, tol, f"{dtype} q{bits} hd{hd} at {at} cap {cap}")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("hd", [32, 128])
+@pytest.mark.parametrize("fq,fk,fv", [(120, -120, 0), (124, -120, -100), (-120, 120, 120), (60, -60, 0)])
+def test_cached_fp32_sizes_far_from_one(bits, hd, fq, fk, fv):
+    """Queries whose products with a code alone would pass fp32, and sizes at the other
+    end, whose scores are ordinary."""
+    B, n, H = 1, 70, 2
+    q = rows((B, 2, H, hd), "f32", 1, 2.0 ** fq)
+    k, v = rows((B, n, H, hd), "f32", 2, 2.0 ** fk), rows((B, n, H, hd), "f32", 3, 2.0 ** fv)
+    q[:, 1] *= 2.0 ** -130 if fq > 100 else 1.0       # one row huge, one small
+    assert torch.isfinite(q).all()
+    for cap in (n, 40000):
+        c = KvCache(B, H, cap, hd, bits=bits)
+        c.write(k.cuda(), v.cuda())
+        for softcap in (0.0, 3.0):
+            got = ops.cached_attention(q.cuda(), c, torch.tensor([n], dtype=torch.int32).cuda(), softcap=softcap)
+            tol = torch.zeros(q.shape, dtype=torch.float64)
+            want = ref.cached(q, k, v, [n], bits, softcap, tol=tol)
+            ref.check(got, want, tol, f"q{bits} hd{hd} 2^{fq} 2^{fk} 2^{fv} cap {cap} softcap {softcap}")
