@@ -514,7 +514,8 @@ typedef struct gm_scores {
  * count as max_seq).  q and out: [B, Sq, n_heads, head_dim] of `dtype`,
  * n_heads a multiple of cache->heads; query head h reads key head
  * h / (n_heads / cache->heads).  Softmax statistics and sums are fp32; for
- * 16-bit dtypes a probability times a value's scale is rounded to fp16.
+ * 16-bit dtypes a probability times a value's scale is rounded to fp16, and
+ * elements of a query below 2^-24 of its largest lose bits.
  * workspace: device, 16-byte aligned, at least
  * gm_attention_cached_workspace(...) bytes (which may be 0: then NULL will do;
  * 0 too for sizes that the call refuses), used by this call alone until it has

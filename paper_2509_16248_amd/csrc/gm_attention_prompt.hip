@@ -16,8 +16,8 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 
 // One query by one wavefront, a key per lane: two passes over the keys, the
-// largest score, then the sums.  A key of weight 0 is skipped, so that nothing a
-// hidden value holds can reach the sums.
+// largest score, then the sums.  A hidden key is skipped, so that nothing its value
+// holds can reach the sums.
 template <typename T, int HD>
 __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, int h, int i) {
   constexpr int CL = (HD + 63) / 64;   // channels per lane
@@ -272,17 +272,22 @@ constexpr int kTiles = 2048;      // key tiles a workgroup keeps marks for (1310
 // nothing.  For the others wavefront 0 fetches mask and documents with the tile.
 // SPARSE (masks or documents given) holds all of that; without it the kernel is half as
 // long, which 8192 tokens in rows of 128, causal, feel in 57.5 against 46.5 us.
-// Measured, 32 heads of 128, bf16, causal: 2048 tokens 57.7 us (596 TFLOP/s), capped 67.2,
-// biased 65.1, both 77.5; without the causal mask 78.3 (878 TFLOP/s) and 94.0; 8192 tokens
-// and 8 key heads 569 us (966 TFLOP/s), in 7 equal documents 176 (445: tiles that straddle two
-// documents, and workgroups of unequal length).  What bounds
-// a short row is a tile's chain of dependent steps (1.8 us of 2 workgroups a CU where
-// the matrix cores work 0.9) and that its heaviest workgroup has twice the average;
-// vector instructions taken out of the cap (a polynomial) changed nothing.
+// Probabilities are rounded to T for the second product (half a step of each, 2^-9 or
+// 2^-12 of it; their sum takes them unrounded): its operands are 16-bit.
+// Measured, launches one after the other, 32 heads of 128, bf16, causal: 2048 tokens 56.7
+// us (606 TFLOP/s), capped 65.9, biased 60.0, both 69.6; without the causal mask 75.2 us
+// (914 TFLOP/s), capped 94.2; 8192 tokens and 8 key heads 535 us (1028 TFLOP/s), in 7 equal
+// documents 171 (459: tiles that straddle two documents, and workgroups of unequal
+// length).  What bounds a short row is that its heaviest workgroup has twice the average
+// (the capped 2048 tokens: CUs hold work 71% of the time) and a tile's chain of dependent
+// steps, in which at two wavefronts per SIMD the vector units work 60% of that time and
+// the matrix cores 29%; vector instructions taken out of the cap (a polynomial) changed
+// nothing.
 // A hidden key has probability 0, but 0 times an Inf or NaN value is NaN in the
 // matrix product.  Such a product is never finite, so queries whose sums came out
 // not finite are computed again by prompt_row, which skips hidden keys; the loop
-// itself checks nothing.
+// itself checks nothing.  Every query that meets such a value pays a wavefront's walk
+// over its keys: 4 x 1000 tokens, 16 heads of 64, NaN in all padding, 30 us -> 6.9 ms.
 
 // Wavefronts per SIMD: as many as the registers leave room for (two at every head size:
 // 4x2048x32 heads of 64, causal, 116 us; three 98).

@@ -20,7 +20,10 @@ template <typename T> struct Row8 {
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = reinterpret_cast<const u32x4*>(p)[i];
   }
-  __device__ __forceinline__ void store(T* p) const {   // past the caches: read back elsewhere, if at all
+  // Past the caches (1 x 2048 x 32 heads of 128, 4 bits, 10.5 us, plain stores 11.4; 2 x
+  // 3000 x 8 heads 7.9 and 9.5).  An attention that reads the rows next has them from the
+  // Infinity Cache either way: both calls together 56.2 and 55.9, 72.0 and 72.7.
+  __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i) __builtin_nontemporal_store(raw[i], reinterpret_cast<u32x4*>(p) + i);
   }
@@ -601,17 +604,19 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 //    holds are the 8 k slots of its B operand: w needs no exchange.  A row m of product i
 //    is channel (HD / 16) m + i, a lane reading HD / 16 channels of 8 keys.  A lane's own
 //    column counts where the channel's group is the column's.
-// The query is divided by a power of two as well (largest element to 2^14), so that bf16
-// and fp16 rows become fp16 without loss.  The maximum m moves lazily (by more than 2^8).
+// The query is divided by a power of two as well (largest element to 2^14), so that of
+// bf16 and fp16 rows only elements below 2^-24 of the largest lose bits in fp16.  The
+// maximum m moves lazily (by more than 2^8).
 // The tile being worked on and its successor, which arrives meanwhile, are both in
 // registers.
 // Heads with more rows than a set of columns holds (4 of 128 channels) take more
 // workgroups, which read the same codes again, mostly from cache; two sets in one
 // workgroup need 256 registers and gain nothing (16 sequences of 4000 keys, 32/4 heads,
 // 4 bits: 21.8 us a set each, 23.6 two; 8 bits 29.1 and 43.0).
-// Measured: 32 sequences of 8190 keys, 32/8 heads of 128, 4 bits, 67 us (4.5 TB/s; a large
-// copy reaches 4.8; 250 vector instructions per tile); 4 of 8000 keys, 32 heads, 8 bits,
-// 59 us (4.7 TB/s).
+// Measured, launches one after the other: 32 sequences of 8190 keys, 32/8 heads of 128, 4
+// bits, 62 us (4.9 TB/s; a large copy reaches 4.8; 270 vector instructions per tile),
+// capped 73 (300); 4 of 8000 keys, 32 heads, 8 bits, 58 us (4.8 TB/s).  Ragged, capped, the
+// vector units work 73% of the time that CUs hold work, the matrix cores 12%.
 
 // Wavefronts per SIMD that the registers of a tile, its successor and O leave room for.
 constexpr int cached_waves(int hd, int bits) { return hd == 128 ? (bits == 4 ? 3 : 2) : hd == 64 ? 3 : 4; }
