@@ -598,8 +598,8 @@ __device__ __forceinline__ void load_words(const char* p, uint32_t* w) {
 //    addition, exact; taken off the sums it would leave errors of an offset times w).
 //    w = exp2(score - m) * V scale of the column's group, rounded to fp16 after division
 //    by a power of two above the largest weight at the last look and at least an eighth
-//    of any since, and times 2^12 (at most 2^15, so that what falls below fp16's smallest
-//    normal is 2^-25 of the largest weight or less; in units of the largest scale a value
+//    of any since, and times 2^8 (at most 2^11, and 2^15 where the power would pass 2^126, so
+//    that what falls below fp16's smallest normal is 2^-21 of the largest weight or less; in units of the largest scale a value
 //    of no weight would take the bits of all others).  The 8 keys whose scores a lane
 //    holds are the 8 k slots of its B operand: w needs no exchange.  A row m of product i
 //    is channel (HD / 16) m + i, a lane reading HD / 16 channels of 8 keys.  A lane's own
@@ -713,8 +713,8 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
 
   float m = -INFINITY, l = 0.f;
   // the largest weight p * V scale at the last look; one over the power of two above it
-  // (2^-115 to 2^126, so that 2^12 times this is finite)
-  float peak = 0.f, inv_unit = __uint_as_float((127u + 115) << 23);
+  // (2^-119 to 2^126, so that 2^8 times this is finite)
+  float peak = 0.f, inv_unit = __uint_as_float((127u + 119) << 23);
   auto unit_of = [](float inv) { return __uint_as_float((254u << 23) - __float_as_uint(inv)); };
   f32x4 o[NI];
 #pragma unroll
@@ -805,14 +805,14 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
       peak = fminf(fmaxf(peak * f, most), 3.4028234e38f);   // (a product past fp32: its largest)
       const uint32_t e = __float_as_uint(peak) >> 23;
       f *= unit_of(inv_unit);                       // (old / new unit alone may pass fp32)
-      inv_unit = __uint_as_float((e < 11 ? 242 : e > 252 ? 1 : 253 - e) << 23);
+      inv_unit = __uint_as_float((e < 7 ? 246 : e > 252 ? 1 : 253 - e) << 23);
       f *= inv_unit;
 #pragma unroll
       for (int e2 = 0; e2 < NI; ++e2) o[e2] *= f;
     }
     f16x8 wf;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) wf[j] = static_cast<_Float16>(s[j] * (sv[j] * (4096.f * inv_unit)));
+    for (int j = 0; j < 8; ++j) wf[j] = static_cast<_Float16>(s[j] * (sv[j] * (256.f * inv_unit)));
     // ---- O += V w: word j of product e holds keys 2 j (low half) and 2 j + 1
     if constexpr (BITS == 4) {
 #pragma unroll
@@ -867,7 +867,7 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int x = 0; x < NI; ++x) {
-        const float unit = BITS == 4 && x % 2 ? 256.f : 4096.f;   // 2^20 or 2^24, over 2^12
+        const float unit = BITS == 4 && x % 2 ? 4096.f : 65536.f;   // 2^20 or 2^24, over 2^8
         s_o[wave][n / NG][NI * (4 * g + e) + x] =
             l == 0.f ? 0.f : (o[x][e] * unit * inv) * unit_of(inv_unit);
       }
@@ -883,14 +883,16 @@ void k_cached_mfma(gm_cached_attention a, gm_kv_cache c, CachedPlan plan) {
     float M = -INFINITY, L = 0.f, O = 0.f;
 #pragma unroll
     for (int x = 0; x < NWV; ++x) M = fmaxf(M, s_m[x][row]);
+    float f[NWV];
 #pragma unroll
     for (int x = 0; x < NWV; ++x) {
-      const float f = s_m[x][row] == -INFINITY && s_l[x][row] == 0.f
-                          ? 0.f : s_l[x][row] * __builtin_amdgcn_exp2f(s_m[x][row] - M);
-      L += f;
-      O += f == 0.f ? 0.f : f * s_o[x][row][ch];
+      f[x] = s_m[x][row] == -INFINITY && s_l[x][row] == 0.f
+                 ? 0.f : s_l[x][row] * __builtin_amdgcn_exp2f(s_m[x][row] - M);
+      L += f[x];
     }
-    O = L == 0.f ? 0.f : O / L;
+    const float inv = L == 0.f ? 0.f : 1.f / L;   // (before the products, which might pass fp32)
+#pragma unroll
+    for (int x = 0; x < NWV; ++x) O += f[x] == 0.f ? 0.f : f[x] * inv * s_o[x][row][ch];
     if (plan.nsplit == 1) {
       cached_out<T>(a, c, w.b, w.kvh, gr)[ch] = from_f32<T>(O);
     } else {

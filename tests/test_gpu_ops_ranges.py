@@ -201,3 +201,28 @@ def test_cached_fp32_sizes_far_from_one(bits, hd, fq, fk, fv):
             tol = torch.zeros(q.shape, dtype=torch.float64)
             want = ref.cached(q, k, v, [n], bits, softcap, tol=tol)
             ref.check(got, want, tol, f"q{bits} hd{hd} 2^{fq} 2^{fk} 2^{fv} cap {cap} softcap {softcap}")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("signs", [False, True])
+def test_cached_values_near_the_largest_number(bits, hd, signs):
+    """bf16 values near the end of the range, whose averages are finite, under scores
+    that rise by less than a move of the running maximum and by more."""
+    B, n, H = 1, 600, 2
+    q = torch.full((B, 1, H, hd), hd ** -0.5).bfloat16()
+    v = 3.2e38 - 1e37 * rows((B, n, H, hd), "f32", 3).abs().clamp(max=3.0)
+    if signs:
+        v = v * torch.sign(rows((B, n, H, hd), "f32", 4))
+    v = v.bfloat16()
+    for rise in (0.0, 5.0, 40.0):
+        # a score is k's average times scale hd = hd ** 0.5 times it: from 0 to `rise`
+        k = (torch.linspace(0, rise, n)[None, :, None, None] + rows((B, n, H, hd), "f32", 2, 0.1)).bfloat16()
+        for cap in (n, 40000):                    # one chunk, and several with a merge
+            c = KvCache(B, H, cap, hd, bits=bits)
+            c.write(k.cuda(), v.cuda())
+            got = ops.cached_attention(q.cuda(), c, torch.tensor([n], dtype=torch.int32).cuda(), scale=hd ** -0.5)
+            tol = torch.zeros(q.shape, dtype=torch.float64)
+            want = ref.cached(q, k, v, [n], bits, scale=hd ** -0.5, tol=tol)
+            assert torch.isfinite(want.bfloat16()).all()
+            ref.check(got, want, tol, f"q{bits} hd{hd} rise {rise} cap {cap}")
