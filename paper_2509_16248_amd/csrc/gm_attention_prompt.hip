@@ -15,9 +15,10 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// One query by one wavefront, a key per lane: two passes over the keys, the
-// largest score, then the sums.  A hidden key is skipped, so that nothing its value
-// holds can reach the sums.
+// One query by one wavefront, a key per lane: two passes over the keys, the largest
+// score and the weights' sum, then the output, of weights that add up to 1, so that
+// it overflows only where it has to.  A hidden key is skipped, so that nothing its
+// value holds can reach the sums.
 template <typename T, int HD>
 __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, int h, int i) {
   constexpr int CL = (HD + 63) / 64;   // channels per lane
@@ -45,19 +46,26 @@ __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, 
     for (int c = 0; c < HD; ++c) s = fmaf(to_f32(q[c]), to_f32(k[c]), s);
     return modify_score(s * a.scores.scale, a.scores.softcap, slope, fabsf(static_cast<float>(qpos - j)));
   };
-  float m = -INFINITY;
-  for (int j0 = 0; j0 < kend; j0 += 64)
-    if (visible(j0 + lane)) m = fmaxf(m, score(j0 + lane));
-  m = wave_max(m);
-  float l = 0.f, o[CL] = {};
+  float m = -INFINITY, l = 0.f;
+  for (int j0 = 0; j0 < kend; j0 += 64) {
+    if (!visible(j0 + lane)) continue;
+    const float x = score(j0 + lane);
+    if (x == -INFINITY) continue;
+    const float mn = fmaxf(m, x);
+    l = (m == -INFINITY ? l : l * expf(m - mn)) + expf(x - mn);   // (a NaN stays)
+    m = mn;
+  }
+  const float M = wave_max(m);
+  l = wave_sum(m == -INFINITY ? l : l * expf(m - M));
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  float o[CL] = {};
   for (int j0 = 0; j0 < kend; j0 += 64) {
     const bool ok = visible(j0 + lane);
     float p = 0.f;
     if (ok) {
-      const float s = score(j0 + lane);
-      p = s == -INFINITY ? 0.f : expf(s - m);
+      const float x = score(j0 + lane);
+      p = x == -INFINITY ? 0.f : expf(x - M) * inv;
     }
-    l += p;
     const unsigned long long on = __ballot(ok);
     for (int t = 0; t < 64 && j0 + t < kend; ++t) {
       const float pt = __shfl(p, t, 64);
@@ -68,11 +76,10 @@ __device__ __forceinline__ void prompt_row(const gm_prompt_attention& a, int b, 
         if (lane + 64 * c < HD) o[c] = fmaf(pt, to_f32(v[lane + 64 * c]), o[c]);
     }
   }
-  l = wave_sum(l);
   T* out = static_cast<T*>(a.out.p) + b * a.out.batch + i * a.out.token + h * a.out.head;
 #pragma unroll
   for (int c = 0; c < CL; ++c)
-    if (lane + 64 * c < HD) out[lane + 64 * c] = from_f32<T>(l == 0.f ? 0.f : o[c] / l);
+    if (lane + 64 * c < HD) out[lane + 64 * c] = from_f32<T>(l == 0.f ? 0.f : o[c]);
 }
 
 // ------------------------------------------------------------ fp32
@@ -220,16 +227,16 @@ void k_prompt_f32(gm_prompt_attention a) {
     float M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < NW; ++w) M = fmaxf(M, s_m[w][i]);
-    float L = 0.f, O = 0.f;
-    if (M != -INFINITY)
+    float L = 0.f, O = 0.f, f[NW];
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float f = s_m[w][i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][i] - M);
-        L += s_l[w][i] * f;
-        O += s_o[w][c][i] * f;
-      }
-    static_cast<float*>(a.out.p)[b * a.out.batch + (q0 + i) * a.out.token + h * a.out.head + c] =
-        L > 0.f ? O / L : 0.f;
+    for (int w = 0; w < NW; ++w) {
+      f[w] = s_m[w][i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w][i] - M);
+      L += s_l[w][i] * f[w];
+    }
+    const float inv = L > 0.f ? 1.f / L : 0.f;   // (before the sum, which might pass fp32)
+#pragma unroll
+    for (int w = 0; w < NW; ++w) O += s_o[w][c][i] * (f[w] * inv);
+    static_cast<float*>(a.out.p)[b * a.out.batch + (q0 + i) * a.out.token + h * a.out.head + c] = O;
   }
   if (__builtin_expect(again != 0, 0))
     for (int i = wave; i < 32; i += NW)

@@ -226,3 +226,23 @@ def test_cached_values_near_the_largest_number(bits, hd, signs):
             want = ref.cached(q, k, v, [n], bits, scale=hd ** -0.5, tol=tol)
             assert torch.isfinite(want.bfloat16()).all()
             ref.check(got, want, tol, f"q{bits} hd{hd} rise {rise} cap {cap}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("softcap", [0.0, 20.0])
+def test_prompt_values_near_the_largest_number(dtype, hd, softcap):
+    """Values whose sum passes fp32 and whose average does not, next to queries that see
+    nothing and under masks."""
+    B, S, H = 2, 150, 2
+    q, k = rows((B, S, H, hd), dtype, 1), rows((B, S, H, hd), dtype, 2)
+    v = (3.2e38 - 1e37 * rows((B, S, H, hd), "f32", 3).abs().clamp(max=3.0)).to(ref.DT[dtype])
+    v[1] = (v[1].float() * torch.sign(rows((S, H, hd), "f32", 4))).to(ref.DT[dtype])
+    mask = torch.ones(B, S, dtype=torch.int32)
+    mask[0, :20], mask[1, 90:] = 0, 0
+    v[1, 100, :, 3] = float("nan")                    # hidden
+    got = ops.attention(q.cuda(), k.cuda(), v.cuda(), causal=True, softcap=softcap, key_mask=mask.cuda())
+    tol = torch.zeros(q.shape, dtype=torch.float64)
+    want = ref.prompt(q, k, v, causal=True, softcap=softcap, key_mask=mask, tol=tol)
+    assert torch.isfinite(want.to(ref.DT[dtype])).all() and not want[0, :20].any()
+    ref.check(got, want, tol, f"{dtype} hd{hd} cap {softcap}")
