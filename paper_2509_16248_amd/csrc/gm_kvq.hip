@@ -415,6 +415,12 @@ __device__ __forceinline__ float* cached_part(const gm_cached_attention& a, cons
   return static_cast<float*>(a.workspace) + (row * p.nsplit + split) * (HD + 2);
 }
 
+// 1 / x of a sum of weights (0, or 1 and more), 0 for 0: refined once, shorter than a division.
+__device__ __forceinline__ float over_sum(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  return x == 0.f ? 0.f : fmaf(fmaf(-x, r, 1.f), r, r);
+}
+
 // One query row by a workgroup.  HD / 8 lanes hold a key row, 8 channels each; every
 // lane group keeps an online softmax of its own, merged by shuffles and in LDS.
 template <typename T, int HD, int BITS>
@@ -463,7 +469,9 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
       x[j] = static_cast<float>(static_cast<int>(code) - OFF);
     }
   };
-  float m = -INFINITY, l = 0.f, o[8];
+  // o is in units of 1 / fit: 1, or 2^32 once the group has met a scale above 2^90, whose
+  // sums might pass fp32
+  float m = -INFINITY, l = 0.f, o[8], fit = 1.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) o[j] = 0.f;
   // U keys a lane group, their rows loaded together (keys past the end read the
@@ -499,7 +507,14 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
       for (int off = G / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
       if (key >= k1 || !on[u]) continue;       // the same for the whole lane group
       s = modify_score(s * scale, a.scores.softcap, slope, static_cast<float>(qpos - key));
-      const float mn = fmaxf(m, s), sv = bf16_value(vscale[u]);
+      const float mn = fmaxf(m, s);
+      float sv = bf16_value(vscale[u]) * fit;
+      if (__builtin_expect(sv > 0x1p90f && fit == 1.f, 0)) {
+        fit = 0x1p-32f;
+        sv *= fit;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] *= fit;
+      }
       const float corr = m == mn ? 1.f : expf(m - mn), p = s == -INFINITY ? 0.f : expf(s - mn);
       l = l * corr + p;
 #pragma unroll
@@ -507,16 +522,21 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
       m = mn;
     }
   }
+  // the lane groups' outputs, divided by their sums before they are joined
+  const float own = over_sum(l) * (fit == 1.f ? 1.f : 0x1p32f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o[j] *= own;
 #pragma unroll
   for (int off = G; off < 64; off <<= 1) {
     const float mo = __shfl_xor(m, off, 64), lo = __shfl_xor(l, off, 64);
     const float mm = fmaxf(m, mo);
-    const float w0 = m == -INFINITY ? 0.f : expf(m - mm);
-    const float w1 = mo == -INFINITY ? 0.f : expf(mo - mm);
-    l = l * w0 + lo * w1;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = o[j] * w0 + __shfl_xor(o[j], off, 64) * w1;
+    const float w0 = l * (m == -INFINITY ? 0.f : expf(m - mm));
+    const float w1 = lo * (mo == -INFINITY ? 0.f : expf(mo - mm));
+    l = w0 + w1;
     m = mm;
+    const float inv = over_sum(l);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = o[j] * (w0 * inv) + __shfl_xor(o[j], off, 64) * (w1 * inv);
   }
   if (lane < G) {
     if (lane == 0) {
@@ -531,12 +551,13 @@ __global__ __launch_bounds__(256) void k_cached_rows(gm_cached_attention a, gm_k
   if (ch >= HD) return;
   float M = -INFINITY, L = 0.f, O = 0.f;
   for (int x = 0; x < NWV; ++x) M = fmaxf(M, s_m[x]);
+  float f[NWV];
   for (int x = 0; x < NWV; ++x) {
-    const float f = s_m[x] == -INFINITY ? 0.f : expf(s_m[x] - M);
-    L += s_l[x] * f;
-    O += s_o[x][ch] * f;
+    f[x] = s_l[x] * (s_m[x] == -INFINITY ? 0.f : expf(s_m[x] - M));
+    L += f[x];
   }
-  O = L == 0.f ? 0.f : O / L;
+  const float inv = over_sum(L);
+  for (int x = 0; x < NWV; ++x) O += s_o[x][ch] * (f[x] * inv);
   if (plan.nsplit == 1) {
     cached_out<T>(a, c, w.b, w.kvh, w.blk)[ch] = from_f32<T>(O);
     return;

@@ -246,3 +246,25 @@ def test_prompt_values_near_the_largest_number(dtype, hd, softcap):
     want = ref.prompt(q, k, v, causal=True, softcap=softcap, key_mask=mask, tol=tol)
     assert torch.isfinite(want.to(ref.DT[dtype])).all() and not want[0, :20].any()
     ref.check(got, want, tol, f"{dtype} hd{hd} cap {softcap}")
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("signs", [False, True])
+def test_cached_fp32_values_near_the_largest_number(bits, hd, signs):
+    """As the bf16 test above, and where only some sequences, groups or keys are so large."""
+    B, n, H = 2, 300, 2
+    q, k = rows((B, 2, H, hd), "f32", 1), rows((B, n, H, hd), "f32", 2)
+    v = 3.2e38 - 1e37 * rows((B, n, H, hd), "f32", 3).abs().clamp(max=3.0)
+    if signs:
+        v = v * torch.sign(rows((B, n, H, hd), "f32", 4))
+    v[1, :150] *= 1e-30                               # later keys large
+    v[1, :, :, hd - 32:] *= 2.0 ** -100               # a group of ordinary size
+    for cap in (n, 40000):                            # one chunk, and several with a merge
+        c = KvCache(B, H, cap, hd, bits=bits)
+        c.write(k.cuda(), v.cuda())
+        got = ops.cached_attention(q.cuda(), c, torch.tensor([n, 290], dtype=torch.int32).cuda())
+        tol = torch.zeros(q.shape, dtype=torch.float64)
+        want = ref.cached(q, k, v, [n, 290], bits, tol=tol)
+        assert torch.isfinite(want.float()).all()
+        ref.check(got, want, tol, f"q{bits} hd{hd} cap {cap}")
