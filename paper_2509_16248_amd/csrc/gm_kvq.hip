@@ -346,7 +346,11 @@ struct CachedPlan {
 // saves the merge's launch (one chunk / split: 8 sequences, 12 heads of 64, 8 bits,
 // capacity 1024, length 300 6.7 / 8.3, 640 8.1 / 9.1, 1000 10.5 / 10.4; capacity 2048, 2000
 // 16.1 / 11.0; one, 32 heads of 128, 4 bits, capacity 256 6.4 / 7.9, 512 8.0 / 7.9, 1024
-// 12.0 / 8.6): a call knows the capacity, a cache in use is half full on average.  The
+// 12.0 / 8.6): a call knows the capacity, a cache in use is half full on average.  Above it,
+// 8 wavefronts in the one chunk: 8 x 12 heads of 64, 8 bits, capacity 1280, half full / full
+// 7.2 / 10.1 against 8.3 / 10.9 split, 1792 8.2 / 12.0 against 10.4 / 12.1; one, 32 heads of
+// 64, 4 bits, 1280 6.7 / 9.2 against 7.7 / 8.2, 1792 7.6 / 11.1 against 7.9 / 8.2; 4, 32/8 heads
+// of 128, 8 bits, 640 7.8 / 10.4 against 8.6 / 8.9, 1024 9.4 / 13.3 against 8.7 / 9.6.  The
 // fp32 kernel, one row a workgroup, wants 1024 of them (8 sequences of 2000 keys, 32/8
 // heads of 128, at 256 / 512 / 1024 / 2048: 60.6 / 43.2 / 37.6 / 38.7) and half the positions
 // (one, 12 heads of 64, capacity 1024, length 300 7.6 / 7.3, 1000 15.7 / 7.5).
