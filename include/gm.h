@@ -442,8 +442,9 @@ int gm_flush_effects(gm_model *m, gm_effect_cb cb, void *user, int32_t *n_droppe
 /* ------------------------------------------------------------ operators
  * Attention and KV-cache operators on caller tensors, without a model: a
  * cache held in 8 or 4 bits (gm_kv_write, gm_kv_read), attention of new
- * tokens over it (gm_attention_cached), and attention over whole prompts with
- * modified scores (gm_attention).  A model created with gm_model_create_ex
+ * tokens over it (gm_attention_cached), attention over whole prompts with
+ * modified scores (gm_attention); and a cache in pages (gm_paged_append) with
+ * attention over it (gm_paged_attention).  A model created with gm_model_create_ex
  * runs the same kernels.  They only enqueue on `stream`: no host
  * synchronisation, no allocation, capturable.  All pointers are device
  * pointers of the current device; a bad argument that the host can see gives
@@ -532,6 +533,82 @@ typedef struct gm_cached_attention {
 int gm_attention_cached(const gm_cached_attention* a, hipStream_t stream);
 uint64_t gm_attention_cached_workspace(const gm_kv_cache* cache, int32_t dtype, int32_t B,
                                        int32_t Sq, int32_t n_heads);
+
+/* Keys and values of many sequences in pages of page_size tokens, in the type
+ * of the model: k and v [pages][heads][page_size][head_dim] of `dtype`, 16-byte
+ * aligned.  page_size is a power of two from 16 to 256, head_dim 32, 64 or 128.
+ * Which pages belong to which sequence is a table's matter (gm_paged_rows). */
+typedef struct gm_paged_cache {
+  int32_t dtype, pages, page_size, heads, head_dim;
+  void *k, *v;
+} gm_paged_cache;
+
+/* The new tokens of a call and where they belong.  Their tensors are
+ * [B, n, heads, head_dim], n tokens a sequence; or, with offsets (int32 [B + 1],
+ * ascending), packed: [n, heads, head_dim] with n rows in all (a gm_tensor whose
+ * `batch` is not looked at), rows offsets[b] .. offsets[b + 1] - 1 being sequence
+ * b's and rows of no sequence neither read nor written.
+ *  lengths  int32 [B]: tokens of each sequence, the new ones included: token i
+ *           of n_b new ones is at position lengths[b] - n_b + i
+ *  table    int32 [B, width], rows table_stride elements apart: position p of
+ *           sequence b is slot p % page_size of page table[b][p / page_size].  An
+ *           entry that is no page (outside [0, pages)) is a hole: nothing is
+ *           stored there and nobody sees its positions.  Entries past a
+ *           sequence's length are not followed.
+ * width * page_size positions, at most 2^24, are what a sequence can hold; a
+ * token at a negative position, as where lengths[b] < n_b, belongs nowhere.
+ * All arrays are read on the device. */
+typedef struct gm_paged_rows {
+  int32_t B, n, width;
+  int64_t table_stride;
+  const int32_t *table, *lengths, *offsets;
+} gm_paged_rows;
+
+/* Store the new tokens' keys and values, and rotate by position on the way: with
+ * rot > 0 (a multiple of 16, at most head_dim) and h = rot / 2, channel c < h of
+ * a key at position p becomes x[c] cos[p][c] - x[c + h] sin[p][c] and channel
+ * c + h x[c + h] cos[p][c] + x[c] sin[p][c], in fp32, rounded once; the channels
+ * from rot on, and the values, are stored as they are.  cos and sin: fp32
+ * [positions][rot / 2], 16-byte aligned, positions >= width * page_size.
+ * Rows of no place (a hole, a position outside the table) are not stored.  Two
+ * rows that fall on one place (sequences that share a page) race.
+ * With n_q_heads > 0 the queries q (n_q_heads heads) are rotated into q_out, which
+ * may be q itself; rows at positions outside the table become zeros.  k, v and q
+ * are of cache->dtype. */
+typedef struct gm_paged_append_args {
+  const gm_paged_cache* cache;
+  gm_paged_rows rows;
+  gm_tensor k, v;
+  int32_t n_q_heads, rot;
+  gm_tensor q, q_out;
+  const float *cos, *sin;
+  int64_t positions;
+} gm_paged_append_args;
+int gm_paged_append(const gm_paged_append_args* a, hipStream_t stream);
+
+/* Attention of the new tokens over the cache, which already holds them: a token
+ * at position p sees the positions up to p that lie below the sequence's length and
+ * in no hole; with window > 0 only those above p - window.  One that sees nothing
+ * gives zeros, and what a hidden key or value holds, Inf and NaN among it, does not
+ * reach it.  q and out: n_heads heads of cache->dtype, n_heads a multiple of
+ * cache->heads, query head h reading key head h / (n_heads / cache->heads).
+ * Scores, softmax statistics and sums are fp32; 16-bit probabilities are rounded
+ * to the type.
+ * workspace: device, 16-byte aligned, at least gm_paged_attention_workspace(...)
+ * bytes (which may be 0: then NULL will do; 0 too for sizes that the call
+ * refuses), used by this call alone until it has run.  `packed`: with offsets. */
+typedef struct gm_paged_attention_args {
+  const gm_paged_cache* cache;
+  gm_paged_rows rows;
+  int32_t n_heads, window;
+  gm_tensor q, out;
+  gm_scores scores;
+  void* workspace;
+  uint64_t workspace_bytes;
+} gm_paged_attention_args;
+int gm_paged_attention(const gm_paged_attention_args* a, hipStream_t stream);
+uint64_t gm_paged_attention_workspace(const gm_paged_cache* cache, int32_t B, int32_t n,
+                                      int32_t width, int32_t n_heads, int32_t packed);
 
 /* The cache of one layer of a model with kv_bits, for gm_kv_read (inspection,
  * handing a sequence's rows over).  To be read only: the model keeps its

@@ -32,7 +32,8 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", f"--offload-arch={ARCH}",
 SOURCES = ([("gm_gemm_16bit.hip", {"GM_T": t, "GM_GROUP": g}) for t in (0, 1) for g in range(4)]
            + [(s, {}) for s in ("gm_rows.hip", "gm_gemm.hip", "gm_gemm_f32.hip",
                                 "gm_gemm_skinny.hip", "gm_attention.hip", "gm_decode.hip",
-                                "gm_kvq.hip", "gm_attention_prompt.hip", "gm_ops.cpp",
+                                "gm_kvq.hip", "gm_attention_prompt.hip", "gm_paged.hip",
+                                "gm_paged_prompt.hip", "gm_ops.cpp",
                                 "gm_runtime.cpp")])
 
 

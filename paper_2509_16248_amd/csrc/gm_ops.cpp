@@ -104,6 +104,58 @@ bool cached_fits(int B, int Sq, int n_heads) {
   return static_cast<double>(B) * Sq * n_heads < 16777216.0;
 }
 
+// The query rows of a call over pages fit a launch.
+bool paged_fits(int B, int n, int n_heads, bool packed) {
+  const double tokens = packed ? static_cast<double>(n) + B : static_cast<double>(B) * n;
+  return tokens * n_heads < 16777216.0;
+}
+
+int check_paged_cache(const gm_paged_cache* c) {
+  if (!c) return inval("cache is NULL");
+  if (int rc = check_dtype(c->dtype)) return rc;
+  if (int rc = check_head_dim(c->head_dim)) return rc;
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)))
+    return inval("page_size must be a power of two from 16 to 256");
+  if (c->pages < 1 || c->heads < 1 || c->heads > (1 << 16))
+    return inval("cache pages and heads must be positive");
+  if (!c->k || !c->v) return inval("a cache pointer is NULL");
+  if (misaligned(c->k, 16) || misaligned(c->v, 16)) return inval("cache memory must be 16-byte aligned");
+  return GM_OK;
+}
+
+// Sizes alone: what the workspace depends on.
+int check_paged_sizes(const gm_paged_cache* c, int B, int n, int width) {
+  if (int rc = check_paged_cache(c)) return rc;
+  if (B < 0 || B > (1 << 20)) return inval("B must be at most 2^20");
+  if (n < 0 || n >= kPositions) return inval("n must be below 2^24");
+  if (width < 1 || static_cast<int64_t>(width) * c->page_size > kPositions)
+    return inval("the table's width times page_size must be positive and at most 2^24");
+  return GM_OK;
+}
+
+int check_paged_rows(const gm_paged_cache* c, const gm_paged_rows& r) {
+  if (int rc = check_paged_sizes(c, r.B, r.n, r.width)) return rc;
+  if (!r.offsets && static_cast<double>(r.B) * r.n >= kPositions) return inval("B * n must be below 2^24");
+  if (r.B == 0 || r.n == 0) return GM_OK;
+  if (!r.table || !r.lengths) return inval("table or lengths is NULL");
+  if (misaligned(r.table, 4) || misaligned(r.lengths, 4) || misaligned(r.offsets, 4))
+    return inval("int32 arrays must be 4-byte aligned");
+  if (r.B > 1 && (r.table_stride < 0 || r.table_stride >= (int64_t(1) << 40)))
+    return inval("table_stride is out of range");
+  return GM_OK;
+}
+
+// The tensors of new tokens: packed ones are one sequence of n.
+int check_paged_tensor(const gm_tensor& t, const gm_paged_cache* c, const gm_paged_rows& r, int heads,
+                       bool output) {
+  return check_tensor(t, c->dtype, r.offsets ? 1 : r.B, r.n, heads, c->head_dim, output);
+}
+
+bool same_place(const gm_tensor& x, const gm_tensor& y, const gm_paged_rows& r, int heads) {
+  return x.p == y.p && (r.offsets || r.B == 1 || x.batch == y.batch) && (r.n == 1 || x.token == y.token) &&
+         (heads == 1 || x.head == y.head);
+}
+
 int launched() {
   HIP_TRY(hipGetLastError());
   return GM_OK;
@@ -190,6 +242,69 @@ int gm_attention(const gm_prompt_attention* a, hipStream_t stream) {
   if (a->out.p == a->q.p || (a->Sk > 0 && (a->out.p == a->k.p || a->out.p == a->v.p)))
     return inval("out and an input overlap");
   launch_attention_prompt(*a, stream);
+  return launched();
+}
+
+int gm_paged_append(const gm_paged_append_args* a, hipStream_t stream) {
+  if (!a) return inval("arguments are NULL");
+  const gm_paged_cache* c = a->cache;
+  const gm_paged_rows& r = a->rows;
+  int rc = check_paged_rows(c, r);
+  if (rc || (rc = check_paged_tensor(a->k, c, r, c->heads, false)) ||
+      (rc = check_paged_tensor(a->v, c, r, c->heads, false)))
+    return rc;
+  if (a->n_q_heads < 0 || a->n_q_heads > (1 << 16)) return inval("n_q_heads must be from 0 to 2^16");
+  if (a->n_q_heads > 0 && ((rc = check_paged_tensor(a->q, c, r, a->n_q_heads, false)) ||
+                           (rc = check_paged_tensor(a->q_out, c, r, a->n_q_heads, true))))
+    return rc;
+  if (a->rot < 0 || a->rot > c->head_dim || a->rot % 16)
+    return inval("rot must be 0 or a multiple of 16 up to head_dim");
+  if (r.B == 0 || r.n == 0) return GM_OK;
+  if (a->rot > 0) {
+    if (!a->cos || !a->sin || misaligned(a->cos, 16) || misaligned(a->sin, 16))
+      return inval("cos and sin must be 16-byte aligned pointers");
+    if (a->positions < static_cast<int64_t>(r.width) * c->page_size)
+      return inval("cos and sin must hold every position of the table (width * page_size)");
+  }
+  for (const void* t : {a->k.p, a->v.p})
+    if (t == c->k || t == c->v) return inval("k or v and the cache overlap");
+  if (a->n_q_heads > 0) {
+    const void* o = a->q_out.p;
+    if (o == a->k.p || o == a->v.p || o == c->k || o == c->v) return inval("q_out and another tensor overlap");
+    if (o == a->q.p && !same_place(a->q, a->q_out, r, a->n_q_heads))
+      return inval("q_out may be q itself, not another view of it");
+  }
+  launch_paged_append(*a, stream);
+  return launched();
+}
+
+uint64_t gm_paged_attention_workspace(const gm_paged_cache* cache, int32_t B, int32_t n, int32_t width,
+                                      int32_t n_heads, int32_t packed) {
+  if (check_paged_sizes(cache, B, n, width) || B < 1 || n < 1 || n_heads < 1 || n_heads % cache->heads ||
+      !paged_fits(B, n, n_heads, packed != 0))
+    return 0;
+  return paged_attention_workspace(*cache, B, n, width, n_heads, packed != 0);
+}
+
+int gm_paged_attention(const gm_paged_attention_args* a, hipStream_t stream) {
+  if (!a) return inval("arguments are NULL");
+  const gm_paged_cache* c = a->cache;
+  const gm_paged_rows& r = a->rows;
+  int rc = check_paged_rows(c, r);
+  if (rc || (rc = check_scores(a->scores))) return rc;
+  if (a->n_heads < 1 || a->n_heads % c->heads) return inval("n_heads must be a multiple of the cache's heads");
+  if (a->window < 0 || a->window > kPositions) return inval("window must be 0 (none) or up to 2^24");
+  if ((rc = check_paged_tensor(a->q, c, r, a->n_heads, false)) ||
+      (rc = check_paged_tensor(a->out, c, r, a->n_heads, true)))
+    return rc;
+  if (r.B == 0 || r.n == 0) return GM_OK;
+  if (!paged_fits(r.B, r.n, a->n_heads, r.offsets != nullptr))
+    return inval("the query rows (tokens * n_heads, and sequences * n_heads if packed) must be below 2^24");
+  if (a->out.p == a->q.p || a->out.p == c->k || a->out.p == c->v) return inval("out and an input overlap");
+  const uint64_t need = paged_attention_workspace(*c, r.B, r.n, r.width, a->n_heads, r.offsets != nullptr);
+  if (need && (!a->workspace || misaligned(a->workspace, 16) || a->workspace_bytes < need))
+    return inval("workspace is NULL, misaligned or smaller than gm_paged_attention_workspace");
+  launch_paged_attention(*a, stream);
   return launched();
 }
 

@@ -24,6 +24,10 @@ void launch_kv_read(const gm_kv_cache& c, int dtype, int B, int n, const int32_t
 void launch_attention_cached(const gm_cached_attention& a, hipStream_t s);
 uint64_t attention_cached_workspace(const gm_kv_cache& c, int dtype, int B, int Sq, int n_heads);
 void launch_attention_prompt(const gm_prompt_attention& a, hipStream_t s);
+void launch_paged_append(const gm_paged_append_args& a, hipStream_t s);
+void launch_paged_attention(const gm_paged_attention_args& a, hipStream_t s);
+uint64_t paged_attention_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads,
+                                   bool packed);
 
 // softcap * tanh(s / softcap) - slope * distance of a scaled score, in fp32.
 __device__ __forceinline__ float modify_score(float s, float softcap, float slope, float distance) {

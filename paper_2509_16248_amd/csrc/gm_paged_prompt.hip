@@ -1,0 +1,480 @@
+// gm_paged_prompt.hip -- attention of prompts and chunks of prompts over a paged
+// KV cache (gm.h, gm_paged_attention), 16-bit types.
+#include <math.h>
+
+#include <algorithm>
+
+#include "gm_device.h"
+#include "gm_paged.h"
+
+namespace gm {
+
+namespace {
+
+// Row r of key head kvh of a sequence: token r / G, query head kvh * G + r % G, so that the
+// heads of a group share a workgroup's keys.
+struct PromptPlan {
+  int G;
+  int blocks;     // blocks of 128 rows of a key head; 0: packed, each sequence has its own
+  int most;       // blocks of all sequences at the most
+  int few;        // sequences of at most this many rows are another kernel's
+  int nsplit;     // parts the keys of a block are cut into at the most
+};
+
+constexpr int kRows = 128, kKeys = 64;   // a workgroup's rows, keys of a tile
+constexpr int kLeastTiles = 8;           // tiles a part has at the least
+
+// A workgroup's block of rows, and the keys it goes through.
+struct PromptPlace {
+  int b, kvh, qb, split;                 // b = -1: none
+  long long item;                        // which (block, key head) of the call
+  PagedSeq s;
+  int rows;                              // of the sequence's key heads
+  int qmin, qmax;                        // positions of the block's first and last row
+  int k0, k1, parts;                     // keys, from a multiple of 64; parts that the block has
+};
+__device__ __forceinline__ PromptPlace prompt_place(const gm_paged_attention_args& a, const gm_paged_cache& c,
+                                                    const PromptPlan& p, int block, int kvh, int split) {
+  PromptPlace w;
+  w.kvh = kvh;
+  w.split = split;
+  w.item = static_cast<long long>(block) * c.heads + kvh;
+  int qb;                                // counted from the first row
+  if (p.blocks) {
+    // (later tokens, which see more keys, first; sequences in turn)
+    const int x = block / a.rows.B;
+    w.b = block - x * a.rows.B;
+    qb = p.blocks - 1 - x;
+    w.s = paged_seq(a, c, w.b);
+  } else {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    w.b = -1;
+    for (int b0 = 0; b0 < a.rows.B; b0 += 64) {
+      int nb = 0;
+      if (b0 + lane < a.rows.B) {
+        const int rows = paged_seq(a, c, b0 + lane).n * p.G;
+        nb = rows > p.few ? (rows + kRows - 1) / kRows : 0;
+      }
+      int sum = nb;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += y;
+      }
+      const unsigned long long hit = __ballot(block < before + sum && block >= before + sum - nb);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        w.b = b0 + l;
+        qb = __builtin_amdgcn_readlane(sum, l) + before - 1 - block;   // (the last block first)
+        break;
+      }
+      before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    if (w.b < 0) return w;
+    w.b = __builtin_amdgcn_readfirstlane(w.b);
+    w.s = paged_seq(a, c, w.b);
+  }
+  w.qb = __builtin_amdgcn_readfirstlane(qb);
+  w.rows = w.s.n * p.G;
+  const int last = (w.qb + 1) * kRows < w.rows ? (w.qb + 1) * kRows - 1 : w.rows - 1;
+  w.qmin = w.s.p0 + w.qb * kRows / p.G;
+  w.qmax = w.s.p0 + last / p.G;
+  w.k0 = a.window > 0 && w.qmin - a.window + 1 > 0 ? (w.qmin - a.window + 1) & ~(kKeys - 1) : 0;
+  w.k1 = w.qmax + 1 < w.s.kend ? w.qmax + 1 : w.s.kend;
+  const int tiles = w.k1 > w.k0 ? (w.k1 - w.k0 + kKeys - 1) / kKeys : 0;
+  w.parts = 1;
+  if (p.nsplit > 1 && tiles >= 2 * kLeastTiles) {
+    const int want = tiles / kLeastTiles < p.nsplit ? tiles / kLeastTiles : p.nsplit;
+    const int per = (tiles + want - 1) / want;
+    w.parts = (tiles + per - 1) / per;
+    w.k0 += split * per * kKeys;
+    const int end = w.k0 + per * kKeys;
+    w.k1 = w.k1 < end ? w.k1 : end;
+  }
+  return w;
+}
+
+template <int HD>
+__device__ __forceinline__ float* prompt_part(const gm_paged_attention_args& a, const PromptPlan& p, const PromptPlace& w,
+                                              int split) {
+  return static_cast<float*>(a.workspace) + (w.item * p.nsplit + split) * kRows * (HD + 2);
+}
+
+constexpr int paged_prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 : 4; }
+
+// Workgroup = 128 query rows of one (sequence, key head), as k_prompt_flash
+// (gm_attention_prompt.hip) splits and multiplies: 4 wavefronts x 32 rows, key and value
+// tiles of 64 keys double-buffered in LDS, S^T = K Q^T and O^T += V^T P^T on 32x32x16, a
+// lane holding 32 scores of one row per tile, the running maximum moved lazily.
+// A copy instruction fills 4, 8 or 16 rows, which lie in one page (pages are multiples of
+// 16): the page comes from a word per lane, the tile's 64 table entries, read a tile
+// ahead, and the entries that are no page give the tile's holes in a ballot.  Rows past
+// the last key repeat it.
+// A hidden key has probability 0, but 0 times an Inf or NaN value is NaN in the matrix
+// product: rows whose sums came out not finite are computed again by paged_row, which skips
+// hidden keys.
+template <typename T, int HD, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(paged_prompt_waves(HD), paged_prompt_waves(HD))))
+void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan) {
+  constexpr int KB = kKeys, NW = 4;
+  typedef typename Mfma32A<T>::vec vec;
+  constexpr int KS = HD / 16;                 // k steps of S^T (head dim)
+  constexpr int CB = HD / 32;                 // 32-channel blocks of O^T
+  constexpr int CPR = HD / 8;                 // 16-byte chunks per key row
+  constexpr int RPL = 16 / CPR;               // key rows per 256 bytes
+  constexpr int RPI = 64 / CPR;               // key rows per 1 KB copy instruction
+  constexpr int LPW = KB / RPI / NW;          // copy instructions per wavefront, tile and operand
+  constexpr int TILE = KB * HD;
+  __shared__ __attribute__((aligned(1024))) T sK0[TILE];
+  __shared__ __attribute__((aligned(1024))) T sK1[TILE];
+  __shared__ __attribute__((aligned(1024))) T sV0[TILE];
+  __shared__ __attribute__((aligned(1024))) T sV1[TILE];
+
+  // heads fastest: the blocks of a key head come to one XCD where the heads are a
+  // multiple of 8
+  int x = blockIdx.x;
+  const int kvh = x % c.heads;
+  x /= c.heads;
+  const PromptPlace w = prompt_place(a, c, plan, x / plan.nsplit, kvh, x % plan.nsplit);
+  if (w.b < 0 || w.split >= w.parts) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l32 = lane & 31, h2 = lane >> 5;
+  const int rw0 = w.qb * kRows + wave * 32;   // first row of this wavefront
+  const bool some = rw0 < w.rows;
+  const int rlast = rw0 + 31 < w.rows ? rw0 + 31 : w.rows - 1;
+  const int wmin = w.s.p0 + rw0 / plan.G, wmax = some ? w.s.p0 + rlast / plan.G : wmin - 1;
+  const int r = rw0 + l32, rc = r < w.rows ? r : w.rows - 1;
+  const int qi = rc / plan.G, h = kvh * plan.G + rc - qi * plan.G;
+  const int qpos = w.s.p0 + qi;
+  const int window = a.window > 0 ? a.window : 1 << 30;
+  const int lg = 31 - __builtin_clz(c.page_size), in_page = c.page_size - 1;
+  const int32_t* table = a.rows.table + w.b * a.rows.table_stride;
+  const int kend = w.k1, last_key = kend - 1, last_page = a.rows.width - 1;
+
+  vec qf[KS];
+  {
+    const T* qp = paged_row_at<const T>(a.q, a.rows, w.b, w.s.row0, qi, h);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const vec*>(qp + 16 * ks + 8 * h2);
+  }
+  const float c2 = CAP ? a.scores.scale * (2.f * kPagedLog2e) / a.scores.softcap : a.scores.scale * kPagedLog2e;
+  const float capc = a.scores.softcap * kPagedLog2e;
+  const float slope2 = BIAS ? a.scores.slopes[h] * -kPagedLog2e : 0.f;
+  constexpr bool LOG2 = CAP || BIAS;          // scores are in log2 units before their maximum is taken
+
+  float mrun = -INFINITY, lrun = 0.f;
+  f32x16 oacc[CB];
+#pragma unroll
+  for (int e = 0; e < CB; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[e][i] = 0.f;
+
+  // the table entry of key kb + lane
+  auto entries = [&](int kb) {
+    const int at = (kb + lane) >> lg;
+    return table[at < last_page ? at : last_page];
+  };
+  // swizzles: chunk e of key row r sits at chunk position e ^ f(r) (k_flash)
+  const int cr = lane / CPR, cpos = lane % CPR;
+  // the tile at kb, whose entries are ids; its keys that are in no hole are returned
+  auto issue = [&](int kb, int ids, T* dk, T* dv) {
+    const bool ok = static_cast<unsigned>(ids) < static_cast<unsigned>(c.pages);
+    const int id = ok ? ids : 0;
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+      const int row = (wave * LPW + j) * RPI;
+      const int first = kb + row < (last_key & ~(RPI - 1)) ? kb + row : last_key & ~(RPI - 1);
+      const int64_t at = paged_base(c, __builtin_amdgcn_readlane(id, first - kb), kvh) + (first & in_page) * HD;
+      const int in = first + cr < last_key ? cr : last_key - first;
+      const int fk = ((row + cr) / RPL) % CPR, fv = 4 * (((row + cr) / RPL) % (CPR / 4));
+      dma16(static_cast<const T*>(c.k) + at + in * HD + 8 * (cpos ^ fk), dk + row * HD);
+      dma16(static_cast<const T*>(c.v) + at + in * HD + 8 * (cpos ^ fv), dv + row * HD);
+    }
+    return __ballot(ok);
+  };
+  const int kswz = (l32 / RPL) % CPR;
+  const int g = lane >> 4, e4 = (lane & 15) >> 2, q4 = lane & 3;
+  const int vrow = 4 * (g >> 1) + e4;
+  const int vswz4 = (vrow / RPL) % (CPR / 4);
+  const int vsub = 2 * (g & 1) + (q4 >> 1);
+  const int vin = 4 * (q4 & 1);
+  uint32_t vaddr[CB];
+#pragma unroll
+  for (int e = 0; e < CB; ++e) vaddr[e] = 2 * (vrow * HD + 8 * (4 * (e ^ vswz4) + vsub) + vin);
+
+  unsigned long long there[2] = {0, 0};       // keys of the stages' tiles that are in no hole
+  int ids = 0;                                // entries of the tile after the next
+  // one key tile from stage BUF (the other stage receives the next one)
+  auto tile = [&](auto BUF, int kb) {
+    constexpr int buf = decltype(BUF)::value;
+    T* sk = buf ? sK1 : sK0;
+    T* sv = buf ? sV1 : sV0;
+    wait_vmcnt0();                            // this wavefront's copies of the tile landed
+    __syncthreads();
+    if (kb + KB < kend) {
+      there[buf ^ 1] = issue(kb + KB, ids, buf ? sK0 : sK1, buf ? sV0 : sV1);
+      ids = entries(kb + 2 * KB);
+    }
+    // no key of the tile is seen by this wavefront's rows
+    if (kb > wmax || kb + KB - 1 <= wmin - window) return;
+    const unsigned long long bits = there[buf] & (kend - kb >= KB ? ~0ull : (1ull << (kend - kb)) - 1);
+    // ---- S^T = K Q^T: two 32-key blocks
+    f32x16 sacc[2];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sacc[kk][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const vec kf = *reinterpret_cast<const vec*>(sk + (32 * kk + l32) * HD + 8 * ((2 * ks + h2) ^ kswz));
+        sacc[kk] = Mfma32A<T>::run(kf, qf[ks], sacc[kk]);
+      }
+    }
+    // ---- capped scores, in log2 units
+    if constexpr (CAP) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float e = __builtin_amdgcn_exp2f(sacc[kk][i] * c2) + 1.f;
+          sacc[kk][i] = fmaf(-2.f * capc, __builtin_amdgcn_rcpf(e), capc);
+        }
+    }
+    if constexpr (BIAS) {
+      const float dist = static_cast<float>(qpos - kb - 4 * h2);
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sacc[kk][i] = fmaf(slope2, dist - static_cast<float>(32 * kk + 8 * (i >> 2) + (i & 3)),
+                             CAP ? sacc[kk][i] : sacc[kk][i] * c2);
+    }
+    // ---- masks
+    if (bits != ~0ull || kb + KB - 1 > wmin || kb <= wmax - window) {
+      const int n = qpos + 1 - kb, low = n - window;   // keys [low, n) of the tile
+      unsigned long long vis = bits & (n >= KB ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1);
+      vis &= low <= 0 ? ~0ull : low >= KB ? 0ull : ~((1ull << low) - 1);
+      vis >>= 4 * h2;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sacc[kk][i] = (vis >> (32 * kk + 8 * (i >> 2) + (i & 3))) & 1ull ? sacc[kk][i] : -INFINITY;
+    }
+    // fp16 probabilities times 2^7 (at most 2^15): fewer fall below its smallest normal
+    constexpr float kUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sacc[kk][i]);
+    float mt = LOG2 ? mx : mx * c2;
+    if (__ballot(mt > mrun + kTau)) {          // move the maximum (wavefront-uniform)
+      mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+      const float mnew = fmaxf(mrun, mt);
+      const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+      lrun *= alpha;
+#pragma unroll
+      for (int e = 0; e < CB; ++e) oacc[e] *= alpha;
+      mrun = mnew;
+    }
+    const float msub = mrun == -INFINITY ? 0.f : mrun - kUp;
+    // ---- probabilities, their sum, and P^T as 16-bit B operands
+    vec pb[4];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float s0 = sacc[kk][8 * hf + 2 * j], s1 = sacc[kk][8 * hf + 2 * j + 1];
+          const float p0 = __builtin_amdgcn_exp2f(LOG2 ? s0 - msub : fmaf(s0, c2, -msub));
+          const float p1 = __builtin_amdgcn_exp2f(LOG2 ? s1 - msub : fmaf(s1, c2, -msub));
+          lrun += p0 + p1;
+          v[j] = pack2<T>(p0, p1);
+        }
+        pb[2 * kk + hf] = __builtin_bit_cast(vec, v);
+      }
+    }
+    // ---- O^T += V^T P^T: four 16-key steps; the V^T operands of step
+    // k2 + 1 are read while step k2 multiplies
+    const uint32_t vb = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_vptr)sv));
+    u32x2 vf[2][CB][2];
+    auto vread = [&](auto K2, u32x2 (&dst)[CB][2]) {
+      constexpr int k2 = decltype(K2)::value;
+#pragma unroll
+      for (int e = 0; e < CB; ++e) {
+        dst[e][0] = lds_read_tr16<(16 * k2) * HD * 2>(vb + vaddr[e]);
+        dst[e][1] = lds_read_tr16<(16 * k2 + 8) * HD * 2>(vb + vaddr[e]);
+      }
+    };
+    auto vmul = [&](int k2, u32x2 (&src)[CB][2]) {
+#pragma unroll
+      for (int e = 0; e < CB; ++e) {
+        u32x4 v;
+        v[0] = src[e][0][0]; v[1] = src[e][0][1]; v[2] = src[e][1][0]; v[3] = src[e][1][1];
+        oacc[e] = Mfma32A<T>::run(__builtin_bit_cast(vec, v), pb[k2], oacc[e]);
+      }
+    };
+    vread(std::integral_constant<int, 0>(), vf[0]);
+    vread(std::integral_constant<int, 1>(), vf[1]);
+    lgkm_wait<2 * CB>(&vf[0][0][0], 2 * CB);
+    vmul(0, vf[0]);
+    vread(std::integral_constant<int, 2>(), vf[0]);
+    lgkm_wait<2 * CB>(&vf[1][0][0], 2 * CB);
+    vmul(1, vf[1]);
+    vread(std::integral_constant<int, 3>(), vf[1]);
+    lgkm_wait<2 * CB>(&vf[0][0][0], 2 * CB);
+    vmul(2, vf[0]);
+    lgkm_wait<0>(&vf[1][0][0], 2 * CB);
+    vmul(3, vf[1]);
+  };
+  if (w.k0 < kend) {
+    there[0] = issue(w.k0, entries(w.k0), sK0, sV0);
+    ids = entries(w.k0 + KB);
+    for (int kb = w.k0;; kb += 2 * KB) {
+      tile(std::integral_constant<int, 0>(), kb);
+      if (kb + KB >= kend) break;
+      tile(std::integral_constant<int, 1>(), kb + KB);
+      if (kb + 2 * KB >= kend) break;
+    }
+  }
+  // ---- normalise and store: lane holds channels 32 e + 8 i + 4 (lane / 32) + j of its row
+  const float L = lrun + __shfl_xor(lrun, 32, 64);
+  float odd = 0.f * L;
+#pragma unroll
+  for (int e = 0; e < CB; ++e)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) odd = fmaf(oacc[e][i], 0.f, odd);
+  const unsigned long long odd_lanes = __ballot(odd != 0.f);   // (NaN != 0)
+  uint32_t again = static_cast<uint32_t>(odd_lanes) | static_cast<uint32_t>(odd_lanes >> 32);
+  float* part = w.parts > 1 ? prompt_part<HD>(a, plan, w, w.split) + wave * 32 * (HD + 2) : nullptr;
+  if (r < w.rows && !(again >> l32 & 1)) {
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    if (part) {
+      float* o = part + l32 * (HD + 2);
+      if (h2 == 0) *reinterpret_cast<f32x2*>(o) = f32x2{mrun, L};
+#pragma unroll
+      for (int e = 0; e < CB; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            *reinterpret_cast<f32x2*>(o + 2 + 32 * e + 8 * i + 4 * h2 + 2 * j) =
+                f32x2{oacc[e][4 * i + 2 * j] * inv, oacc[e][4 * i + 2 * j + 1] * inv};
+    } else {
+      T* out = paged_row_at<T>(a.out, a.rows, w.b, w.s.row0, qi, h);
+#pragma unroll
+      for (int e = 0; e < CB; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x2 r2;
+          r2[0] = pack2<T>(oacc[e][4 * i] * inv, oacc[e][4 * i + 1] * inv);
+          r2[1] = pack2<T>(oacc[e][4 * i + 2] * inv, oacc[e][4 * i + 3] * inv);
+          *reinterpret_cast<u32x2*>(out + 32 * e + 8 * i + 4 * h2) = r2;
+        }
+    }
+  }
+  for (; __builtin_expect(again != 0, 0); again &= again - 1) {
+    const int j = __builtin_ctz(again), row = rw0 + j;
+    if (row >= w.rows) break;
+    const int i = row / plan.G, hh = kvh * plan.G + row - i * plan.G;
+    T* out = paged_row_at<T>(a.out, a.rows, w.b, w.s.row0, i, hh);
+    const f32x2 ml = paged_row<T, HD>(a, c, w.s, w.b, hh, i, w.k0, w.k1, [&](int ch, float v) {
+      if (part) part[j * (HD + 2) + 2 + ch] = v;
+      else out[ch] = from_f32<T>(v);
+    });
+    if (part && lane == 0) {
+      part[j * (HD + 2)] = ml[0];
+      part[j * (HD + 2) + 1] = ml[1];
+    }
+  }
+}
+
+// The parts of a block's rows joined in order of their keys: 4 rows a workgroup, a
+// wavefront each.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_prompt_join(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan) {
+  int x = blockIdx.x;
+  const int row = (x % (kRows / 4)) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  x /= kRows / 4;
+  const int kvh = x % c.heads;
+  const PromptPlace w = prompt_place(a, c, plan, x / c.heads, kvh, 0);
+  if (w.b < 0 || w.parts < 2) return;
+  const int r = w.qb * kRows + row;
+  if (r >= w.rows) return;
+  const float* part = prompt_part<HD>(a, plan, w, 0) + row * (HD + 2);
+  const int64_t step = static_cast<int64_t>(kRows) * (HD + 2);
+  const bool on = lane < w.parts;
+  const float m = on ? part[lane * step] : -INFINITY, l = on ? part[lane * step + 1] : 0.f;
+  const float M = wave_max(m);
+  float f = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - M);
+  const float F = wave_sum(f);
+  f = f == 0.f ? 0.f : f / F;
+  const int i = r / plan.G;
+  T* out = paged_row_at<T>(a.out, a.rows, w.b, w.s.row0, i, kvh * plan.G + r - i * plan.G);
+#pragma unroll
+  for (int ch = lane; ch < HD; ch += 64) {
+    float o = 0.f;
+    for (int p = 0; p < w.parts; ++p) {
+      const float fp = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), p));
+      o += fp == 0.f ? 0.f : fp * part[p * step + 2 + ch];
+    }
+    out[ch] = from_f32<T>(o);
+  }
+}
+
+PromptPlan prompt_plan(const gm_paged_cache& c, int B, int n, int width, int n_heads, bool packed, int few) {
+  PromptPlan p;
+  p.G = n_heads / c.heads;
+  p.few = few;
+  const int64_t rows = static_cast<int64_t>(n) * p.G;      // of a key head
+  p.blocks = packed ? 0 : static_cast<int>((rows + kRows - 1) / kRows);
+  p.most = packed ? static_cast<int>(rows / kRows) + B : p.blocks * B;
+  // parts that bring 512 workgroups, where the table holds so many tiles
+  const int64_t full = (packed ? (rows + kRows - 1) / kRows : p.most) * static_cast<int64_t>(c.heads);
+  const int64_t tiles = static_cast<int64_t>(width) * c.page_size / kKeys;
+  int64_t want = full >= 256 ? 1 : 512 / full;
+  want = std::min<int64_t>(want, tiles / kLeastTiles);
+  p.nsplit = static_cast<int>(want < 1 ? 1 : want > 16 ? 16 : want);
+  return p;
+}
+
+}  // namespace
+
+uint64_t paged_prompt_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, bool packed) {
+  const PromptPlan p = prompt_plan(c, B, n, width, n_heads, packed, 0);
+  if (p.nsplit == 1) return 0;
+  return static_cast<uint64_t>(p.most) * c.heads * p.nsplit * kRows * (c.head_dim + 2) * sizeof(float);
+}
+
+void launch_paged_prompt(const gm_paged_attention_args& a, int few, hipStream_t s) {
+  const gm_paged_cache& c = *a.cache;
+  const PromptPlan p = prompt_plan(c, a.rows.B, a.rows.n, a.rows.width, a.n_heads, a.rows.offsets != nullptr, few);
+  const bool cap = a.scores.softcap > 0.f, bias = a.scores.slopes;
+  const std::true_type yes;
+  const std::false_type no;
+  by_paged_cache(c, [&](auto t, auto hd) {
+    typedef decltype(t) T;
+    if constexpr (!std::is_same<T, float>::value) {
+      constexpr int HD = decltype(hd)::value;
+      auto go = [&](auto cp, auto bi) {
+        hipLaunchKernelGGL((k_paged_prompt<T, HD, decltype(cp)::value, decltype(bi)::value>),
+                           dim3(static_cast<unsigned>(p.most) * c.heads * p.nsplit), dim3(256), 0, s, a, c, p);
+      };
+      if (cap && bias) go(yes, yes);
+      else if (cap) go(yes, no);
+      else if (bias) go(no, yes);
+      else go(no, no);
+      if (p.nsplit > 1)
+        hipLaunchKernelGGL((k_paged_prompt_join<T, HD>), dim3(static_cast<unsigned>(p.most) * c.heads * (kRows / 4)),
+                           dim3(256), 0, s, a, c, p);
+    }
+  });
+}
+
+}  // namespace gm

@@ -115,6 +115,29 @@ class gm_cached_attention(ctypes.Structure):
                 ("scores", gm_scores), ("workspace", _vp), ("workspace_bytes", _u64)]
 
 
+class gm_paged_cache(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("pages", _i32), ("page_size", _i32), ("heads", _i32),
+                ("head_dim", _i32), ("k", _vp), ("v", _vp)]
+
+
+class gm_paged_rows(ctypes.Structure):
+    _fields_ = [("B", _i32), ("n", _i32), ("width", _i32), ("table_stride", _i64), ("table", _vp),
+                ("lengths", _vp), ("offsets", _vp)]
+
+
+class gm_paged_append_args(ctypes.Structure):
+    _fields_ = [("cache", ctypes.POINTER(gm_paged_cache)), ("rows", gm_paged_rows),
+                ("k", gm_tensor), ("v", gm_tensor), ("n_q_heads", _i32), ("rot", _i32),
+                ("q", gm_tensor), ("q_out", gm_tensor), ("cos", _vp), ("sin", _vp),
+                ("positions", _i64)]
+
+
+class gm_paged_attention_args(ctypes.Structure):
+    _fields_ = [("cache", ctypes.POINTER(gm_paged_cache)), ("rows", gm_paged_rows),
+                ("n_heads", _i32), ("window", _i32), ("q", gm_tensor), ("out", gm_tensor),
+                ("scores", gm_scores), ("workspace", _vp), ("workspace_bytes", _u64)]
+
+
 class gm_prompt_attention(ctypes.Structure):
     _fields_ = [("dtype", _i32), ("B", _i32), ("Sq", _i32), ("Sk", _i32), ("n_heads", _i32),
                 ("kv_heads", _i32), ("head_dim", _i32), ("q", gm_tensor), ("k", gm_tensor),
@@ -139,7 +162,8 @@ EXPORTS = ["gm_model_create", "gm_model_destroy", "gm_forward", "gm_forward_ex",
            "gm_check_error", "gm_flush_effects", "gm_debug_buffer", "gm_debug_forward_layers",
            "gm_get_stats", "gm_forward_noalloc",
            "gm_kv_write", "gm_kv_read", "gm_attention_cached", "gm_attention_cached_workspace",
-           "gm_attention", "gm_model_create_ex", "gm_set_segments", "gm_model_kv_cache",
+           "gm_attention", "gm_paged_append", "gm_paged_attention", "gm_paged_attention_workspace",
+           "gm_model_create_ex", "gm_set_segments", "gm_model_kv_cache",
            "gm_strerror",
            "gm_last_error"]
 
@@ -189,15 +213,21 @@ def lib(path: str = LIB_PATH) -> ctypes.CDLL:
     L.gm_attention_cached.argtypes = [ctypes.POINTER(gm_cached_attention), _vp]
     L.gm_attention_cached_workspace.argtypes = [ctypes.POINTER(gm_kv_cache), _i32, _i32, _i32, _i32]
     L.gm_attention.argtypes = [ctypes.POINTER(gm_prompt_attention), _vp]
+    L.gm_paged_append.argtypes = [ctypes.POINTER(gm_paged_append_args), _vp]
+    L.gm_paged_attention.argtypes = [ctypes.POINTER(gm_paged_attention_args), _vp]
+    L.gm_paged_attention_workspace.argtypes = [ctypes.POINTER(gm_paged_cache), _i32, _i32, _i32,
+                                               _i32, _i32]
     L.gm_strerror.argtypes = [ctypes.c_int]
     L.gm_strerror.restype = ctypes.c_char_p
     L.gm_last_error.argtypes = []
     L.gm_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("gm_model_destroy", "gm_decisions_device_ptr", "gm_strerror",
-                        "gm_last_error", "gm_attention_cached_workspace"):
+                        "gm_last_error", "gm_attention_cached_workspace",
+                        "gm_paged_attention_workspace"):
             getattr(L, name).restype = ctypes.c_int
     L.gm_attention_cached_workspace.restype = _u64
+    L.gm_paged_attention_workspace.restype = _u64
     _lib = L
     return L
 
@@ -398,3 +428,16 @@ def gm_attention_cached_workspace(cache: gm_kv_cache, dtype: int, B: int, Sq: in
 
 def gm_attention(a: gm_prompt_attention, stream: int) -> None:
     _check(lib().gm_attention(ctypes.byref(a), stream), "gm_attention")
+
+
+def gm_paged_append(a: gm_paged_append_args, stream: int) -> None:
+    _check(lib().gm_paged_append(ctypes.byref(a), stream), "gm_paged_append")
+
+
+def gm_paged_attention(a: gm_paged_attention_args, stream: int) -> None:
+    _check(lib().gm_paged_attention(ctypes.byref(a), stream), "gm_paged_attention")
+
+
+def gm_paged_attention_workspace(cache: gm_paged_cache, B: int, n: int, width: int, n_heads: int,
+                                 packed: bool) -> int:
+    return lib().gm_paged_attention_workspace(ctypes.byref(cache), B, n, width, n_heads, packed)

@@ -1,16 +1,20 @@
 """Attention and KV-cache operators on torch tensors (the operators of gm.h).
 
+:class:`KvCache` (8 or 4 bits, a row of positions a sequence) with
+:func:`cached_attention`; :class:`PagedCache` (the model's type, pages) with
+:func:`paged_attention`; :func:`attention` over whole prompts.
+
 Argument marshalling only, as in :mod:`model`: shapes and dtypes are checked
 here, pointers and the stream go to libgm, which checks the rest and enqueues
 its kernels.  Nothing synchronises; every call can be captured into a graph.
 
-Tensors are ``[batch, tokens, heads, head_dim]`` of float32, bfloat16 or
-float16 on one HIP device.  The channels of a head are contiguous; the base
+Tensors are ``[batch, tokens, heads, head_dim]`` (over pages also packed,
+``[tokens, heads, head_dim]``) of float32, bfloat16 or float16 on one HIP device.  The channels of a head are contiguous; the base
 address and the other strides are multiples of 16 bytes (views of a fused
 q | k | v projection will do).  Work runs on ``stream`` (default: the current
 stream of the tensors' device), and what a call allocates belongs to it;
 tensors made on another stream have to be ready there.  ``out`` may not overlap
-an input.  Forward only: results carry no gradient.
+an input (only ``q_out`` of an append may be ``q``).  Forward only: results carry no gradient.
 """
 from __future__ import annotations
 
@@ -33,9 +37,13 @@ _DTYPES = {torch.float32: gm.GM_DTYPE_F32, torch.bfloat16: gm.GM_DTYPE_BF16,
 _CACHED = struct.Struct("@P4i" + 2 * "P3q" + "P" + "2fP" + "PQ")
 _PROMPT = struct.Struct("@7i" + 4 * "P3q" + "2i" + "2fP" + "4P")
 _TENSOR = struct.Struct("@P3q")
+_PAGED_APPEND = struct.Struct("@P3iq3P" + 2 * "P3q" + "2i" + 2 * "P3q" + "2Pq")
+_PAGED = struct.Struct("@P3iq3P2i" + 2 * "P3q" + "2fP" + "PQ")
 assert _CACHED.size == ctypes.sizeof(gm.gm_cached_attention)
 assert _PROMPT.size == ctypes.sizeof(gm.gm_prompt_attention)
 assert _TENSOR.size == ctypes.sizeof(gm.gm_tensor)
+assert _PAGED_APPEND.size == ctypes.sizeof(gm.gm_paged_append_args)
+assert _PAGED.size == ctypes.sizeof(gm.gm_paged_attention_args)
 
 
 def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> Tuple[int, int, int, int]:
@@ -259,6 +267,192 @@ def cached_attention(q: torch.Tensor, cache: KvCache, lengths: torch.Tensor, *,
     rc = gm.lib().gm_attention_cached(ctypes.byref(a), _raw_stream(device.index))
     if rc:
         raise gm.GmError(rc, "gm_attention_cached")
+    return out
+
+
+def rotary_table(positions: int, channels: int, base: float = 10000.0,
+                 device="cuda") -> Tuple[torch.Tensor, torch.Tensor]:
+    """(cos, sin), float32 [positions, channels / 2], of the angles
+    p * base^(-2 c / channels), taken in float64: the tables that
+    :meth:`PagedCache.append` rotates ``channels`` channels of a head by."""
+    if positions < 0 or channels < 0 or channels % 2:
+        raise ValueError("positions and channels may not be negative, channels must be even")
+    theta = base ** (-torch.arange(0, channels, 2, dtype=torch.float64) / max(channels, 1))
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * theta
+    return angle.cos().float().to(device), angle.sin().float().to(device)
+
+
+class PagedCache:
+    """Keys and values of many sequences in pages, ``k`` and ``v`` [pages, heads,
+    page_size, head_dim] of the model's type (gm_paged_cache).
+
+    Which pages a sequence has is told with every call: ``table`` int32 [B,
+    width], whose rows need not be next to one another, holds the page of
+    positions i * page_size and on at [b, i]; ``lengths`` int32 [B] counts the
+    tokens of each sequence, the call's new ones included.  An entry that is no page
+    (-1) is a hole: nothing is stored there, nobody attends to it.  New tokens
+    come as [B, n, heads, head_dim], or, with ``offsets`` int32 [B + 1], packed
+    as [tokens, heads, head_dim], rows offsets[b] to offsets[b + 1] of sequence
+    b.  All are read on the device.
+    """
+
+    def __init__(self, pages: int, page_size: int, heads: int, head_dim: int,
+                 dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        self._set(torch.zeros((pages, heads, page_size, head_dim), dtype=dtype, device=device),
+                  torch.zeros((pages, heads, page_size, head_dim), dtype=dtype, device=device))
+
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor) -> "PagedCache":
+        """The cache that lives in these two tensors."""
+        cache = cls.__new__(cls)
+        cache._set(k, v)
+        return cache
+
+    def _set(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype is not v.dtype or k.device != v.device:
+            raise ValueError("k and v must be alike, [pages, heads, page_size, head_dim]")
+        if not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k and v must be contiguous")
+        code = _DTYPES.get(k.dtype)
+        if code is None:
+            raise ValueError(f"k must be float32, bfloat16 or float16, not {k.dtype}")
+        self.pages, self.heads, self.page_size, self.head_dim = k.shape
+        if self.head_dim not in (32, 64, 128):
+            raise ValueError("head_dim must be 32, 64 or 128")
+        if self.page_size not in (16, 32, 64, 128, 256):
+            raise ValueError("page_size must be 16, 32, 64, 128 or 256")
+        if not 1 <= self.pages < 1 << 31 or not 1 <= self.heads <= 1 << 16:
+            raise ValueError("pages and heads must be positive, pages below 2^31, heads at most 2^16")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        self.c = gm.gm_paged_cache(code, self.pages, self.page_size, self.heads, self.head_dim,
+                                   k.data_ptr(), v.data_ptr())
+        self._address = ctypes.addressof(self.c)
+        self._workspace = {}      # bytes that attention needs, by the sizes of a call
+
+    def _rows(self, t, name, tokens, heads):
+        """The fields of a gm_tensor of new tokens, [*tokens, heads, head_dim]."""
+        if t.dtype is not self.dtype:
+            raise ValueError(f"{name} must be {self.dtype}, not {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}, not {t.device}")
+        if t.shape != (*tokens, heads, self.head_dim):
+            raise ValueError(f"{name} must have shape {(*tokens, heads, self.head_dim)}, "
+                             f"not {tuple(t.shape)}")
+        stride = t.stride()
+        if stride[-1] != 1 and t.numel():
+            raise ValueError(f"the channels of {name} must be contiguous")
+        return t.data_ptr(), stride[0] if len(stride) == 4 else 0, stride[-3], stride[-2]
+
+    def _places(self, t, name, table, lengths, offsets):
+        """(the new tokens' shape, the fields of a gm_paged_rows)."""
+        if not self.k.is_cuda:
+            raise ValueError(f"the cache must be on a HIP device, not {self.device}")
+        packed = offsets is not None
+        if t.dim() != (3 if packed else 4):
+            raise ValueError(f"{name} must be [tokens, heads, head_dim] with offsets, "
+                             "[batch, tokens, heads, head_dim] without")
+        if table.dim() != 2 or table.dtype is not torch.int32 or (
+                table.stride(1) != 1 and table.shape[1] > 1):
+            raise ValueError("table must be an int32 tensor [batch, width] with contiguous rows")
+        if table.device != self.device:
+            raise ValueError(f"table must be on {self.device}, not {table.device}")
+        B, width = table.shape
+        tokens = tuple(t.shape[:-2])
+        if not packed and tokens[0] != B:
+            raise ValueError(f"{name} is of {tokens[0]} sequences, the table of {B}")
+        return tokens, (B, tokens[-1], width, table.stride(0), table.data_ptr(),
+                        _ints(lengths, "lengths", (B,), self.device),
+                        _ints(offsets, "offsets", (B + 1,), self.device))
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
+               *, offsets: Optional[torch.Tensor] = None,
+               rotary: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+               q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               stream=None) -> Optional[torch.Tensor]:
+        """Store the new tokens' keys and values (gm_paged_append).
+
+        ``rotary`` is (cos, sin), float32 [positions, r / 2] with a row for every position
+        that the table can hold (:func:`rotary_table`): keys are stored with their
+        first r channels turned by position, channel c with channel c + r / 2.  The
+        queries ``q`` are turned too and returned, in ``q_out`` (which may be ``q``) or a
+        new tensor; rows at positions outside the table become zeros."""
+        if lengths is None:
+            raise ValueError("lengths is missing")
+        device = self.device
+        tokens, places = self._places(k, "k", table, lengths, offsets)
+        cos, sin = rotary if rotary is not None else (None, None)
+        if _elsewhere(device, stream):
+            with _there(device, stream, k, v, table, lengths, offsets, cos, sin, q, q_out, self.k,
+                        self.v):
+                return self.append(k, v, table, lengths, offsets=offsets, rotary=rotary, q=q,
+                                   q_out=q_out)
+        rot = positions = 0
+        if cos is not None:
+            if cos.dim() != 2:
+                raise ValueError("cos must be [positions, r / 2]")
+            positions, rot = cos.shape[0], 2 * cos.shape[1]
+            shape = (positions, rot // 2)
+            cos = _ints(cos, "cos", shape, device, torch.float32)
+            sin = _ints(sin, "sin", shape, device, torch.float32)
+        heads, rows, out = 0, (0, 0, 0, 0), (0, 0, 0, 0)
+        if q is not None:
+            if q.dim() != k.dim():
+                raise ValueError("q must have as many dimensions as k")
+            heads = q.shape[-2]
+            rows = self._rows(q, "q", tokens, heads)
+            if q_out is None:
+                q_out = _empty(q, q.shape)
+            out = self._rows(q_out, "q_out", tokens, heads)
+        elif q_out is not None:
+            raise ValueError("q_out needs q")
+        a = gm.gm_paged_append_args.from_buffer_copy(_PAGED_APPEND.pack(
+            self._address, *places, *self._rows(k, "k", tokens, self.heads),
+            *self._rows(v, "v", tokens, self.heads), heads, rot, *rows, *out, cos or 0, sin or 0,
+            positions))
+        rc = gm.lib().gm_paged_append(ctypes.byref(a), _raw_stream(device.index))
+        if rc:
+            raise gm.GmError(rc, "gm_paged_append")
+        return q_out
+
+
+def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
+                    lengths: torch.Tensor, *, offsets: Optional[torch.Tensor] = None,
+                    window: int = 0, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Attention of the newest tokens q over the cache, which already holds their
+    keys and values (gm_paged_attention): of one or a few tokens a sequence, or
+    of whole prompts and chunks of them.
+
+    ``table``, ``lengths`` and ``offsets`` as in :class:`PagedCache`; a token at
+    position p sees the positions up to p, with ``window`` > 0 only those above p -
+    window, and none in holes; one that sees nothing gives zeros.  ``n_heads``
+    is a multiple of the cache's heads.  Scores as in :func:`cached_attention`."""
+    if lengths is None:
+        raise ValueError("lengths is missing")
+    device = cache.device
+    tokens, places = cache._places(q, "q", table, lengths, offsets)
+    if _elsewhere(device, stream):
+        with _there(device, stream, q, out, table, lengths, offsets, slopes, cache.k, cache.v):
+            return paged_attention(q, cache, table, lengths, offsets=offsets, window=window,
+                                   softcap=softcap, slopes=slopes, scale=scale, out=out)
+    H = q.shape[-2]
+    rows = cache._rows(q, "q", tokens, H)
+    key = (places[0], places[1], places[2], H, offsets is None)
+    need = cache._workspace.get(key)
+    if need is None:
+        need = gm.gm_paged_attention_workspace(cache.c, *key[:4], offsets is not None)
+        cache._workspace[key] = need
+    if out is None:
+        out = _empty(q, q.shape)
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    a = gm.gm_paged_attention_args.from_buffer_copy(_PAGED.pack(
+        cache._address, *places, H, window, *rows, *cache._rows(out, "out", tokens, H),
+        1.0 / math.sqrt(cache.head_dim) if scale is None else scale, softcap,
+        _ints(slopes, "slopes", (H,), device, torch.float32), work.data_ptr() if need else 0, need))
+    rc = gm.lib().gm_paged_attention(ctypes.byref(a), _raw_stream(device.index))
+    if rc:
+        raise gm.GmError(rc, "gm_paged_attention")
     return out
 
 
