@@ -608,7 +608,8 @@ typedef struct gm_paged_attention_args {
 } gm_paged_attention_args;
 int gm_paged_attention(const gm_paged_attention_args* a, hipStream_t stream);
 uint64_t gm_paged_attention_workspace(const gm_paged_cache* cache, int32_t B, int32_t n,
-                                      int32_t width, int32_t n_heads, int32_t packed);
+                                      int32_t width, int32_t n_heads, int32_t window,
+                                      int32_t packed);
 
 /* The cache of one layer of a model with kv_bits, for gm_kv_read (inspection,
  * handing a sequence's rows over).  To be read only: the model keeps its

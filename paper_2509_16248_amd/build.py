@@ -1,8 +1,9 @@
-"""Build libgm.so (the HIP kernels and the C ABI runtime) for gfx950.
+"""Build libgm.so (the HIP kernels and the C ABI runtime) for gfx950, and
+_gm_torch.so (host code: operators called on torch tensors).
 
 Usage: ``python -m paper_2509_16248_amd.build`` or ``build()``.  Objects go
-to ``_build/`` at the repository root; the library is written next to this
-file, where the Python binding loads it from.
+to ``_build/`` at the repository root; the libraries are written next to this
+file, where the Python binding loads them from.
 """
 from __future__ import annotations
 
@@ -11,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,6 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libgm.so")
+TORCH_LIB = os.path.join(PKG, "_gm_torch.so")
 ARCH = os.environ.get("GM_OFFLOAD_ARCH", "gfx950")
 
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
@@ -50,10 +53,42 @@ def _compile(unit) -> str:
     return obj
 
 
+def _compile_torch() -> str:
+    """Object of the module on torch tensors: host code, so the host compiler's."""
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    obj = os.path.join(OBJ, "gm_torch.o")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-fPIC", "-std=c++17", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE,
+           "-isystem", os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(HIPCC))), "include"),
+           "-isystem", sysconfig.get_paths()["include"]]
+    for path in include_paths():
+        cmd += ["-isystem", path]
+    cmd += ["-c", os.path.join(CSRC, "gm_torch.cpp"), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    return obj
+
+
+def _link_torch(obj: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = TORCH_LIB + ".tmp"
+    cmd = [shutil.which("g++") or "g++", "-shared", "-o", tmp, obj, "-L", PKG, "-l:libgm.so",
+           "-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, TORCH_LIB)
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every source and link libgm.so; returns the library path."""
+    """Compile every source and link the libraries; returns the path of libgm.so."""
     os.makedirs(OBJ, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+        torch_obj = ex.submit(_compile_torch)
         objs = list(ex.map(_compile, SOURCES))
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
@@ -61,8 +96,9 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    _link_torch(torch_obj.result())
     if verbose:
-        print(f"built {LIB}")
+        print(f"built {LIB} and {TORCH_LIB}")
     return LIB
 
 

@@ -110,6 +110,10 @@ bool paged_fits(int B, int n, int n_heads, bool packed) {
   return tokens * n_heads < 16777216.0;
 }
 
+int check_window(int window) {
+  return window < 0 || window > kPositions ? inval("window must be 0 (none) or up to 2^24") : GM_OK;
+}
+
 int check_paged_cache(const gm_paged_cache* c) {
   if (!c) return inval("cache is NULL");
   if (int rc = check_dtype(c->dtype)) return rc;
@@ -279,11 +283,11 @@ int gm_paged_append(const gm_paged_append_args* a, hipStream_t stream) {
 }
 
 uint64_t gm_paged_attention_workspace(const gm_paged_cache* cache, int32_t B, int32_t n, int32_t width,
-                                      int32_t n_heads, int32_t packed) {
+                                      int32_t n_heads, int32_t window, int32_t packed) {
   if (check_paged_sizes(cache, B, n, width) || B < 1 || n < 1 || n_heads < 1 || n_heads % cache->heads ||
-      !paged_fits(B, n, n_heads, packed != 0))
+      check_window(window) || !paged_fits(B, n, n_heads, packed != 0))
     return 0;
-  return paged_attention_workspace(*cache, B, n, width, n_heads, packed != 0);
+  return paged_attention_workspace(*cache, B, n, width, n_heads, window, packed != 0);
 }
 
 int gm_paged_attention(const gm_paged_attention_args* a, hipStream_t stream) {
@@ -293,7 +297,7 @@ int gm_paged_attention(const gm_paged_attention_args* a, hipStream_t stream) {
   int rc = check_paged_rows(c, r);
   if (rc || (rc = check_scores(a->scores))) return rc;
   if (a->n_heads < 1 || a->n_heads % c->heads) return inval("n_heads must be a multiple of the cache's heads");
-  if (a->window < 0 || a->window > kPositions) return inval("window must be 0 (none) or up to 2^24");
+  if ((rc = check_window(a->window))) return rc;
   if ((rc = check_paged_tensor(a->q, c, r, a->n_heads, false)) ||
       (rc = check_paged_tensor(a->out, c, r, a->n_heads, true)))
     return rc;
@@ -301,7 +305,7 @@ int gm_paged_attention(const gm_paged_attention_args* a, hipStream_t stream) {
   if (!paged_fits(r.B, r.n, a->n_heads, r.offsets != nullptr))
     return inval("the query rows (tokens * n_heads, and sequences * n_heads if packed) must be below 2^24");
   if (a->out.p == a->q.p || a->out.p == c->k || a->out.p == c->v) return inval("out and an input overlap");
-  const uint64_t need = paged_attention_workspace(*c, r.B, r.n, r.width, a->n_heads, r.offsets != nullptr);
+  const uint64_t need = paged_attention_workspace(*c, r.B, r.n, r.width, a->n_heads, a->window, r.offsets != nullptr);
   if (need && (!a->workspace || misaligned(a->workspace, 16) || a->workspace_bytes < need))
     return inval("workspace is NULL, misaligned or smaller than gm_paged_attention_workspace");
   launch_paged_attention(*a, stream);

@@ -27,7 +27,7 @@ void launch_attention_prompt(const gm_prompt_attention& a, hipStream_t s);
 void launch_paged_append(const gm_paged_append_args& a, hipStream_t s);
 void launch_paged_attention(const gm_paged_attention_args& a, hipStream_t s);
 uint64_t paged_attention_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads,
-                                   bool packed);
+                                   int window, bool packed);
 
 // softcap * tanh(s / softcap) - slope * distance of a scaled score, in fp32.
 __device__ __forceinline__ float modify_score(float s, float softcap, float slope, float distance) {

@@ -50,6 +50,35 @@ __device__ __forceinline__ int64_t paged_base(const gm_paged_cache& c, int page,
   return (static_cast<int64_t>(page) * c.heads + kvh) * c.page_size * c.head_dim;
 }
 
+// The sequence of packed row `row`, by one wavefront: how many end at or before it (B: none
+// holds it; nor does the one found, if it begins behind it).
+__device__ __forceinline__ int paged_sequence_of(const gm_paged_rows& r, int row) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b0 = 0; b0 < r.B; b0 += 64) {
+    const int end = b0 + lane < r.B ? r.offsets[b0 + lane + 1] : row + 1;
+    const int some = __builtin_popcountll(__ballot(end <= row));
+    before += some;
+    if (some < 64) break;
+  }
+  return __builtin_amdgcn_readfirstlane(before);
+}
+
+// Running sum over the lanes, each with those before it (wave_sum's steps).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, ROWS == 0xf);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  v += dpp_or_0<0x111, 0xf>(v);   // row_shr:1
+  v += dpp_or_0<0x112, 0xf>(v);   // row_shr:2
+  v += dpp_or_0<0x114, 0xf>(v);   // row_shr:4
+  v += dpp_or_0<0x118, 0xf>(v);   // row_shr:8
+  v += dpp_or_0<0x142, 0xa>(v);   // row_bcast:15 into rows 1 and 3
+  v += dpp_or_0<0x143, 0xc>(v);   // row_bcast:31 into rows 2 and 3
+  return v;
+}
+
 // One query row (token i of sequence b, head h) over the keys [k0, k1) by one
 // wavefront, a key per lane: two passes over the keys, the largest score and the
 // weights' sum, then the output, of weights that add up to 1, so that it overflows only

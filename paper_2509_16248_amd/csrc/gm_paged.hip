@@ -43,15 +43,7 @@ __global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm
   int b, i, row = blockIdx.x;
   int64_t pos;
   if (r.offsets) {
-    const int lane = threadIdx.x & 63;
-    int before = 0;                          // sequences that end at or before this row
-    for (int b0 = 0; b0 < r.B; b0 += 64) {
-      const int end = b0 + lane < r.B ? r.offsets[b0 + lane + 1] : row + 1;
-      const int some = __builtin_popcountll(__ballot(end <= row));
-      before += some;
-      if (some < 64) break;
-    }
-    b = __builtin_amdgcn_readfirstlane(before);
+    b = paged_sequence_of(r, row);
     if (b >= r.B) return;
     const int o0 = const_load(r.offsets + b), end = const_load(r.offsets + b + 1), o1 = end < r.n ? end : r.n;
     if (row < o0) return;
@@ -152,6 +144,7 @@ struct PagedPlan {
   int few;       // sequences of more rows than this are another kernel's (0: none are)
   int wgs;       // workgroups that share all tiles; 0: a workgroup an item
   int items;     // items there are at the most
+  int joined;    // rows of a (sequence, key head) that the join looks at; 0: by token and head
 };
 
 constexpr int kMostParts = 64;     // workgroups that share an item
@@ -164,6 +157,12 @@ __device__ __forceinline__ void paged_weight(const gm_paged_attention_args& a, c
   // (a sequence without keys still has rows to clear)
   tiles = (s.kend - (s.lo & ~31) + UNIT - 1) / UNIT;
   tiles = tiles > 0 ? tiles : 1;
+}
+
+// Tiles a workgroup takes of all, where an item has at most `most`.
+__device__ __forceinline__ int paged_share(const PagedPlan& p, unsigned all, unsigned most) {
+  const unsigned even = (all + p.wgs - 1) / p.wgs, least = (most + kMostParts - 3) / (kMostParts - 2);
+  return __builtin_amdgcn_readfirstlane(even > least ? even : least);
 }
 
 // Where in the line of all sequences' items and tiles something lies.
@@ -188,23 +187,10 @@ __device__ __forceinline__ PagedFound paged_find(const gm_paged_attention_args& 
     tiles += static_cast<unsigned>(nb) * c.heads * nt;
     most = nb && static_cast<unsigned>(nt) > most ? nt : most;
   }
-  unsigned si = items, st = tiles;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned yi = __shfl_up(si, o, 64), yt = __shfl_up(st, o, 64);
-    if (lane >= o) {
-      si += yi;
-      st += yt;
-    }
-  }
+  const unsigned si = wave_scan(items), st = wave_scan(tiles);
   PagedFound f;
   f.all_tiles = __builtin_amdgcn_readlane(st, 63);
-  f.per = 0;
-  if (p.wgs) {
-    most = wave_max_u32(most);
-    const unsigned even = (f.all_tiles + p.wgs - 1) / p.wgs, least = (most + kMostParts - 3) / (kMostParts - 2);
-    f.per = __builtin_amdgcn_readfirstlane(even > least ? even : least);
-  }
+  f.per = p.wgs ? paged_share(p, f.all_tiles, wave_max_u32(most)) : 0;
   const unsigned at = by_tile ? x * f.per : x;
   const unsigned mine = by_tile ? tiles : items, end = by_tile ? st : si;
   const unsigned long long hit = __ballot(at < end && at >= end - mine);
@@ -617,25 +603,48 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
   }
 }
 
-// The parts of a cut item's row joined, a workgroup per row: the weights by the first
-// wavefront, a lane per part, then the parts in 256 / HD sets, each in order, and the
-// sets in theirs.
+// The parts of a cut item's row joined, a workgroup per row (token and head): the weights
+// by the first wavefront, a lane per part, then the parts in 256 / HD sets, each in order,
+// and the sets in theirs.
 template <typename T, int HD, int R, int UNIT>
 __global__ __launch_bounds__(256) void k_paged_join(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
   constexpr int SETS = 256 / HD;
   __shared__ float s_w[64], s_o[SETS][HD];
-  const int tid = threadIdx.x, ch = tid % HD, of = tid / HD;
-  const unsigned item = blockIdx.x / R;
-  const int row = blockIdx.x - item * R;
-  const PagedFound f = paged_find<R, UNIT>(a, c, plan, item, false);
-  if (f.b < 0) return;
-  const PagedSeq s = paged_seq(a, c, f.b);
+  const int tid = threadIdx.x, ch = tid % HD, of = tid / HD, lane = tid & 63;
+  int b, i = 0, h;
+  if (plan.joined) {
+    const int x = blockIdx.x / plan.joined, r = blockIdx.x - x * plan.joined;
+    b = x / c.heads;
+    i = r / plan.G;
+    h = (x - b * c.heads) * plan.G + r - i * plan.G;
+  } else {
+    const int token = blockIdx.x / a.n_heads;
+    h = blockIdx.x - token * a.n_heads;
+    b = a.rows.offsets ? paged_sequence_of(a.rows, token) : token / a.rows.n;
+    if (b >= a.rows.B) return;
+    i = a.rows.offsets ? token - a.rows.offsets[b] : token - b * a.rows.n;
+  }
+  // ---- tiles of the sequences before this one, and of all
+  unsigned before = 0, all = 0, most = 0;
+  for (int x = lane; x < a.rows.B; x += 64) {
+    int nb, nt;
+    paged_weight<R, UNIT>(a, c, plan, paged_seq(a, c, x), nb, nt);
+    const unsigned t = static_cast<unsigned>(nb) * c.heads * nt;
+    all += t;
+    before += x < b ? t : 0;
+    most = nb && static_cast<unsigned>(nt) > most ? nt : most;
+  }
+  all = __builtin_amdgcn_readlane(wave_scan(all), 63);
+  before = __builtin_amdgcn_readlane(wave_scan(before), 63);
+  const unsigned per = paged_share(plan, all, wave_max_u32(most));
+  const PagedSeq s = paged_seq(a, c, b);
   int nb, nt;
   paged_weight<R, UNIT>(a, c, plan, s, nb, nt);
-  const int x = item - f.items, kvh = x / nb, blk = x - kvh * nb, r = blk * R + row;
-  const unsigned t0 = f.tiles + static_cast<unsigned>(x) * nt;
-  const unsigned w0 = t0 / f.per, w1 = (t0 + nt - 1) / f.per;
-  if (w0 == w1 || r >= s.n * plan.G) return;
+  if (nb == 0 || i < 0 || i >= s.n) return;
+  const int kvh = h / plan.G, r = i * plan.G + h - kvh * plan.G, blk = r / R, row = r - blk * R;
+  const unsigned t0 = before + static_cast<unsigned>(kvh * nb + blk) * nt;
+  const unsigned w0 = t0 / per, w1 = (t0 + nt - 1) / per;
+  if (w0 == w1) return;
   const int parts = w1 - w0 + 1;               // at most kMostParts
   auto part = [&](int p) { return paged_part<R, HD>(a, w0 + p, p == 0, row); };
   constexpr int U = 8;
@@ -675,8 +684,7 @@ __global__ __launch_bounds__(256) void k_paged_join(gm_paged_attention_args a, g
   if (of) return;
 #pragma unroll
   for (int p = 1; p < SETS; ++p) sum += s_o[p][ch];
-  const int i = r / plan.G;
-  paged_row_at<T>(a.out, a.rows, f.b, s.row0, i, kvh * plan.G + r - i * plan.G)[ch] = from_f32<T>(sum);
+  paged_row_at<T>(a.out, a.rows, b, s.row0, i, h)[ch] = from_f32<T>(sum);
 }
 
 // How a call is done.
@@ -689,7 +697,7 @@ struct PagedWay {
 
 constexpr int kFewRows = 32;       // query rows of a key head up to which the rows kernel takes 16 bits
 
-PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads, bool packed) {
+PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads, int window, bool packed) {
   PagedWay w;
   const bool f32 = c.dtype == kF32;
   const int G = n_heads / c.heads;
@@ -702,14 +710,22 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
   p.G = G;
   p.few = w.many ? kFewRows : 0;
   p.blocks = packed ? 0 : static_cast<int>((most + R - 1) / R);
-  // (rows of a packed call lie in at most a block a sequence more than they fill)
-  p.items = c.heads * (packed ? static_cast<int>(most / R) + B : p.blocks * B);
-  w.waves = 4;
-  const int tile = f32 ? 16 : 32;
+  // (rows of a packed call lie in at most a block a sequence more than they fill; where
+  // sequences of more than a block are another kernel's, in one a sequence)
+  p.items = c.heads * (!packed ? p.blocks * B : w.many ? B : static_cast<int>(most / R) + B);
+  p.joined = packed && w.many ? kFewRows : 0;
   const int64_t cap = static_cast<int64_t>(width) * c.page_size;
-  const int64_t tiles = (cap + tile * 4 - 1) / (tile * 4);
+  const int64_t keys = window > 0 ? std::min<int64_t>(cap, static_cast<int64_t>(window) + n) : cap;
+  const int tile = f32 ? 16 : 32;
+  const double item_us = keys * c.head_dim * (f32 ? 8. : 4.) / 46e3, all_us = item_us * p.items * (46e3 / 4.9e6);
   p.wgs = 0;
-  if (p.items < 1024 && tiles > 4) p.wgs = static_cast<int>(std::min<int64_t>(512, tiles * p.items));
+  w.waves = 8;
+  if (p.items > 512 || keys <= 8 * tile) w.waves = 4;
+  if (p.items < 1024 && (item_us > 25. || item_us > all_us + 5.)) {
+    const int64_t tiles = (keys + tile * 4 - 1) / (tile * 4) * p.items;
+    w.waves = tiles >= 512 ? 8 : 4;
+    p.wgs = static_cast<int>(tiles >= 512 ? 256 : tiles);
+  }
   w.rows_bytes = w.few && p.wgs ? static_cast<uint64_t>(p.wgs) * 2 * R * (c.head_dim + 2) * sizeof(float) : 0;
   return w;
 }
@@ -724,8 +740,8 @@ void launch_paged_append(const gm_paged_append_args& a, hipStream_t s) {
   });
 }
 
-uint64_t paged_attention_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, bool packed) {
-  const PagedWay w = paged_way(c, B, n, width, n_heads, packed);
+uint64_t paged_attention_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, int window, bool packed) {
+  const PagedWay w = paged_way(c, B, n, width, n_heads, window, packed);
   // (the two kernels run one after the other)
   const uint64_t many = w.many ? paged_prompt_workspace(c, B, n, width, n_heads, packed) : 0;
   return w.rows_bytes > many ? w.rows_bytes : many;
@@ -733,23 +749,29 @@ uint64_t paged_attention_workspace(const gm_paged_cache& c, int B, int n, int wi
 
 void launch_paged_attention(const gm_paged_attention_args& a, hipStream_t s) {
   const gm_paged_cache& c = *a.cache;
-  const PagedWay w = paged_way(c, a.rows.B, a.rows.n, a.rows.width, a.n_heads, a.rows.offsets != nullptr);
+  const PagedWay w = paged_way(c, a.rows.B, a.rows.n, a.rows.width, a.n_heads, a.window, a.rows.offsets != nullptr);
   if (w.many) launch_paged_prompt(a, w.few ? kFewRows : 0, s);
   if (!w.few) return;
   const PagedPlan p = w.rows;
   by_paged_cache(c, [&](auto t, auto hd) {
     typedef decltype(t) T;
-    constexpr int HD = decltype(hd)::value, NWV = 4;
-    auto go = [&](auto sets, auto cap) {
-      constexpr int NSET = decltype(sets)::value, UNIT = NWV * (sizeof(T) == 4 ? 16 : 32);
+    constexpr int HD = decltype(hd)::value;
+    auto go = [&](auto sets, auto cap, auto waves) {
+      constexpr int NSET = decltype(sets)::value, NWV = decltype(waves)::value, UNIT = NWV * (sizeof(T) == 4 ? 16 : 32);
       hipLaunchKernelGGL((k_paged_rows<T, HD, NSET, decltype(cap)::value, NWV>), dim3(p.wgs ? p.wgs : p.items),
                          dim3(64 * NWV), 0, s, a, c, p);
+      const int tokens = a.rows.offsets ? a.rows.n : a.rows.B * a.rows.n;
+      const int joins = p.joined ? a.rows.B * c.heads * p.joined : tokens * a.n_heads;
       if (p.wgs)
-        hipLaunchKernelGGL((k_paged_join<T, HD, 16 * NSET, UNIT>), dim3(p.items * 16 * NSET), dim3(256), 0, s, a, c, p);
+        hipLaunchKernelGGL((k_paged_join<T, HD, 16 * NSET, UNIT>), dim3(joins), dim3(256), 0, s, a, c, p);
+    };
+    auto wide = [&](auto sets, auto cap) {
+      if (w.waves == 8) go(sets, cap, std::integral_constant<int, 8>());
+      else go(sets, cap, std::integral_constant<int, 4>());
     };
     auto width = [&](auto cap) {
-      if (w.nset == 1) go(std::integral_constant<int, 1>(), cap);
-      else go(std::integral_constant<int, 2>(), cap);
+      if (w.nset == 1) wide(std::integral_constant<int, 1>(), cap);
+      else wide(std::integral_constant<int, 2>(), cap);
     };
     if (a.scores.softcap > 0.f) width(std::true_type());
     else width(std::false_type());

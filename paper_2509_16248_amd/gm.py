@@ -216,7 +216,7 @@ def lib(path: str = LIB_PATH) -> ctypes.CDLL:
     L.gm_paged_append.argtypes = [ctypes.POINTER(gm_paged_append_args), _vp]
     L.gm_paged_attention.argtypes = [ctypes.POINTER(gm_paged_attention_args), _vp]
     L.gm_paged_attention_workspace.argtypes = [ctypes.POINTER(gm_paged_cache), _i32, _i32, _i32,
-                                               _i32, _i32]
+                                               _i32, _i32, _i32]
     L.gm_strerror.argtypes = [ctypes.c_int]
     L.gm_strerror.restype = ctypes.c_char_p
     L.gm_last_error.argtypes = []
@@ -230,6 +230,25 @@ def lib(path: str = LIB_PATH) -> ctypes.CDLL:
     L.gm_paged_attention_workspace.restype = _u64
     _lib = L
     return L
+
+
+_torch_lib = None
+
+
+def torch_lib():
+    """The module of operators on torch tensors, _gm_torch.so (once).  Raises if it is
+    missing, as :func:`lib` does."""
+    global _torch_lib
+    if _torch_lib is None:
+        path = os.path.join(_HERE, "_gm_torch.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built; run __graft_entry__.build()")
+        import importlib
+
+        import torch  # noqa: F401  (the module's libraries)
+        lib()
+        _torch_lib = importlib.import_module(__package__ + "._gm_torch")
+    return _torch_lib
 
 
 class GmError(RuntimeError):
@@ -439,5 +458,6 @@ def gm_paged_attention(a: gm_paged_attention_args, stream: int) -> None:
 
 
 def gm_paged_attention_workspace(cache: gm_paged_cache, B: int, n: int, width: int, n_heads: int,
-                                 packed: bool) -> int:
-    return lib().gm_paged_attention_workspace(ctypes.byref(cache), B, n, width, n_heads, packed)
+                                 window: int, packed: bool) -> int:
+    return lib().gm_paged_attention_workspace(ctypes.byref(cache), B, n, width, n_heads, window,
+                                              packed)

@@ -5,8 +5,8 @@
 :func:`paged_attention`; :func:`attention` over whole prompts.
 
 Argument marshalling only, as in :mod:`model`: shapes and dtypes are checked
-here, pointers and the stream go to libgm, which checks the rest and enqueues
-its kernels.  Nothing synchronises; every call can be captured into a graph.
+here (over pages in a compiled module), pointers and the stream go to libgm, which
+checks the rest and enqueues its kernels.  Nothing synchronises; every call can be captured into a graph.
 
 Tensors are ``[batch, tokens, heads, head_dim]`` (over pages also packed,
 ``[tokens, heads, head_dim]``) of float32, bfloat16 or float16 on one HIP device.  The channels of a head are contiguous; the base
@@ -37,13 +37,9 @@ _DTYPES = {torch.float32: gm.GM_DTYPE_F32, torch.bfloat16: gm.GM_DTYPE_BF16,
 _CACHED = struct.Struct("@P4i" + 2 * "P3q" + "P" + "2fP" + "PQ")
 _PROMPT = struct.Struct("@7i" + 4 * "P3q" + "2i" + "2fP" + "4P")
 _TENSOR = struct.Struct("@P3q")
-_PAGED_APPEND = struct.Struct("@P3iq3P" + 2 * "P3q" + "2i" + 2 * "P3q" + "2Pq")
-_PAGED = struct.Struct("@P3iq3P2i" + 2 * "P3q" + "2fP" + "PQ")
 assert _CACHED.size == ctypes.sizeof(gm.gm_cached_attention)
 assert _PROMPT.size == ctypes.sizeof(gm.gm_prompt_attention)
 assert _TENSOR.size == ctypes.sizeof(gm.gm_tensor)
-assert _PAGED_APPEND.size == ctypes.sizeof(gm.gm_paged_append_args)
-assert _PAGED.size == ctypes.sizeof(gm.gm_paged_attention_args)
 
 
 def _rows(t: torch.Tensor, name: str, shape, dtype, device) -> Tuple[int, int, int, int]:
@@ -90,6 +86,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 @contextlib.contextmanager
 def _there(device, stream, *tensors):
     """The device made current and, if one is given, the stream: what a call
@@ -110,6 +109,7 @@ def _there(device, stream, *tensors):
 
 def _elsewhere(device, stream) -> bool:
     return stream is not None or device.index != torch.cuda.current_device()
+
 
 
 def _tensor(*fields) -> gm.gm_tensor:
@@ -327,42 +327,17 @@ class PagedCache:
         self.c = gm.gm_paged_cache(code, self.pages, self.page_size, self.heads, self.head_dim,
                                    k.data_ptr(), v.data_ptr())
         self._address = ctypes.addressof(self.c)
-        self._workspace = {}      # bytes that attention needs, by the sizes of a call
+        self._index = k.device.index
+        self._scale = 1.0 / math.sqrt(self.head_dim)
+        self._on_gpu = k.is_cuda
+        if self._on_gpu:
+            self._calls = gm.torch_lib()
 
-    def _rows(self, t, name, tokens, heads):
-        """The fields of a gm_tensor of new tokens, [*tokens, heads, head_dim]."""
-        if t.dtype is not self.dtype:
-            raise ValueError(f"{name} must be {self.dtype}, not {t.dtype}")
-        if t.device != self.device:
-            raise ValueError(f"{name} must be on {self.device}, not {t.device}")
-        if t.shape != (*tokens, heads, self.head_dim):
-            raise ValueError(f"{name} must have shape {(*tokens, heads, self.head_dim)}, "
-                             f"not {tuple(t.shape)}")
-        stride = t.stride()
-        if stride[-1] != 1 and t.numel():
-            raise ValueError(f"the channels of {name} must be contiguous")
-        return t.data_ptr(), stride[0] if len(stride) == 4 else 0, stride[-3], stride[-2]
-
-    def _places(self, t, name, table, lengths, offsets):
-        """(the new tokens' shape, the fields of a gm_paged_rows)."""
-        if not self.k.is_cuda:
+    def _away(self, stream) -> bool:
+        """Whether a call has to change the device or the stream."""
+        if not self._on_gpu:
             raise ValueError(f"the cache must be on a HIP device, not {self.device}")
-        packed = offsets is not None
-        if t.dim() != (3 if packed else 4):
-            raise ValueError(f"{name} must be [tokens, heads, head_dim] with offsets, "
-                             "[batch, tokens, heads, head_dim] without")
-        if table.dim() != 2 or table.dtype is not torch.int32 or (
-                table.stride(1) != 1 and table.shape[1] > 1):
-            raise ValueError("table must be an int32 tensor [batch, width] with contiguous rows")
-        if table.device != self.device:
-            raise ValueError(f"table must be on {self.device}, not {table.device}")
-        B, width = table.shape
-        tokens = tuple(t.shape[:-2])
-        if not packed and tokens[0] != B:
-            raise ValueError(f"{name} is of {tokens[0]} sequences, the table of {B}")
-        return tokens, (B, tokens[-1], width, table.stride(0), table.data_ptr(),
-                        _ints(lengths, "lengths", (B,), self.device),
-                        _ints(offsets, "offsets", (B + 1,), self.device))
+        return stream is not None or self._index != _current_device()
 
     def append(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
                *, offsets: Optional[torch.Tensor] = None,
@@ -376,43 +351,17 @@ class PagedCache:
         first r channels turned by position, channel c with channel c + r / 2.  The
         queries ``q`` are turned too and returned, in ``q_out`` (which may be ``q``) or a
         new tensor; rows at positions outside the table become zeros."""
-        if lengths is None:
-            raise ValueError("lengths is missing")
-        device = self.device
-        tokens, places = self._places(k, "k", table, lengths, offsets)
         cos, sin = rotary if rotary is not None else (None, None)
-        if _elsewhere(device, stream):
-            with _there(device, stream, k, v, table, lengths, offsets, cos, sin, q, q_out, self.k,
-                        self.v):
+        if self._away(stream):
+            with _there(self.device, stream, k, v, table, lengths, offsets, cos, sin, q, q_out,
+                        self.k, self.v):
                 return self.append(k, v, table, lengths, offsets=offsets, rotary=rotary, q=q,
                                    q_out=q_out)
-        rot = positions = 0
-        if cos is not None:
-            if cos.dim() != 2:
-                raise ValueError("cos must be [positions, r / 2]")
-            positions, rot = cos.shape[0], 2 * cos.shape[1]
-            shape = (positions, rot // 2)
-            cos = _ints(cos, "cos", shape, device, torch.float32)
-            sin = _ints(sin, "sin", shape, device, torch.float32)
-        heads, rows, out = 0, (0, 0, 0, 0), (0, 0, 0, 0)
-        if q is not None:
-            if q.dim() != k.dim():
-                raise ValueError("q must have as many dimensions as k")
-            heads = q.shape[-2]
-            rows = self._rows(q, "q", tokens, heads)
-            if q_out is None:
-                q_out = _empty(q, q.shape)
-            out = self._rows(q_out, "q_out", tokens, heads)
-        elif q_out is not None:
-            raise ValueError("q_out needs q")
-        a = gm.gm_paged_append_args.from_buffer_copy(_PAGED_APPEND.pack(
-            self._address, *places, *self._rows(k, "k", tokens, self.heads),
-            *self._rows(v, "v", tokens, self.heads), heads, rot, *rows, *out, cos or 0, sin or 0,
-            positions))
-        rc = gm.lib().gm_paged_append(ctypes.byref(a), _raw_stream(device.index))
-        if rc:
+        rc = self._calls.append(self._address, self.k, k, v, table, lengths, offsets, cos, sin, q,
+                                q_out, _raw_stream(self._index))
+        if type(rc) is int:
             raise gm.GmError(rc, "gm_paged_append")
-        return q_out
+        return rc
 
 
 def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
@@ -428,32 +377,16 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
     position p sees the positions up to p, with ``window`` > 0 only those above p -
     window, and none in holes; one that sees nothing gives zeros.  ``n_heads``
     is a multiple of the cache's heads.  Scores as in :func:`cached_attention`."""
-    if lengths is None:
-        raise ValueError("lengths is missing")
-    device = cache.device
-    tokens, places = cache._places(q, "q", table, lengths, offsets)
-    if _elsewhere(device, stream):
-        with _there(device, stream, q, out, table, lengths, offsets, slopes, cache.k, cache.v):
+    if cache._away(stream):
+        with _there(cache.device, stream, q, out, table, lengths, offsets, slopes, cache.k, cache.v):
             return paged_attention(q, cache, table, lengths, offsets=offsets, window=window,
                                    softcap=softcap, slopes=slopes, scale=scale, out=out)
-    H = q.shape[-2]
-    rows = cache._rows(q, "q", tokens, H)
-    key = (places[0], places[1], places[2], H, offsets is None)
-    need = cache._workspace.get(key)
-    if need is None:
-        need = gm.gm_paged_attention_workspace(cache.c, *key[:4], offsets is not None)
-        cache._workspace[key] = need
-    if out is None:
-        out = _empty(q, q.shape)
-    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    a = gm.gm_paged_attention_args.from_buffer_copy(_PAGED.pack(
-        cache._address, *places, H, window, *rows, *cache._rows(out, "out", tokens, H),
-        1.0 / math.sqrt(cache.head_dim) if scale is None else scale, softcap,
-        _ints(slopes, "slopes", (H,), device, torch.float32), work.data_ptr() if need else 0, need))
-    rc = gm.lib().gm_paged_attention(ctypes.byref(a), _raw_stream(device.index))
-    if rc:
+    rc = cache._calls.attention(cache._address, cache.k, q, table, lengths, offsets, window, softcap,
+                                slopes, cache._scale if scale is None else scale, out,
+                                _raw_stream(cache._index))
+    if type(rc) is int:
         raise gm.GmError(rc, "gm_paged_attention")
-    return out
+    return rc
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False,

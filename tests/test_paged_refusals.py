@@ -109,14 +109,14 @@ def test_query_rows_fit_a_launch():
     for r, n_heads in ((dict(B=1 << 12, n=1 << 6), 64), (dict(B=1 << 18, n=100, offsets=P), 64)):
         refused(lambda: gm.gm_paged_attention(attention(r=r, n_heads=n_heads, q=tensor(16 * P, **wide),
                                                         out=tensor(32 * P, **wide)), 0), "below 2^24")
-        assert gm.gm_paged_attention_workspace(cache(), r["B"], r["n"], 5, n_heads, "offsets" in r) == 0
+        assert gm.gm_paged_attention_workspace(cache(), r["B"], r["n"], 5, n_heads, 0, "offsets" in r) == 0
 
 
 @pytest.mark.parametrize("n,packed", [(1, False), (200, False), (200, True), (8, True)])
 @pytest.mark.parametrize("dtype", [0, 1, 2])
 def test_attention_needs_its_workspace(n, packed, dtype):
     c, width = dict(dtype=dtype, heads=1), 4096
-    need = gm.gm_paged_attention_workspace(cache(**c), 1, n, width, 1, packed)
+    need = gm.gm_paged_attention_workspace(cache(**c), 1, n, width, 1, 0, packed)
     assert need > 0
     r = dict(B=1, n=n, width=width, offsets=P if packed else None)
     for workspace, size in ((None, need), (P + 8, need), (P, need - 1)):
@@ -128,14 +128,14 @@ def test_attention_needs_its_workspace(n, packed, dtype):
                                          (-1, 1, 5, 4), (2147483647, 2147483647, 2147483647, 2147483647)])
 def test_workspace_of_sizes_that_the_call_refuses(B, n, width, H):
     for packed in (False, True):
-        assert gm.gm_paged_attention_workspace(cache(), B, n, width, H, packed) == 0
+        assert gm.gm_paged_attention_workspace(cache(), B, n, width, H, 0, packed) == 0
 
 
 def test_null_arguments_and_nothing_to_do():
     L = gm.lib()
     assert L.gm_paged_append(None, None) == gm.GM_E_INVAL
     assert L.gm_paged_attention(None, None) == gm.GM_E_INVAL
-    assert L.gm_paged_attention_workspace(None, 1, 1, 1, 1, 0) == 0
+    assert L.gm_paged_attention_workspace(None, 1, 1, 1, 1, 0, 0) == 0
     none = tensor(p=None)
     for r in (dict(B=0, table=None, lengths=None), dict(n=0, table=None, lengths=None)):
         gm.gm_paged_append(append(r=r, k=none, v=none, q=none, q_out=none, cos=None), 0)
@@ -157,11 +157,6 @@ def test_wrappers_refuse_bad_caches():
         ops.rotary_table(4, 3, device="cpu")
 
 
-class Cuda(torch.Tensor):
-    """A host tensor that says it is on a device: what is refused before any launch."""
-    is_cuda = True
-
-
 def test_wrappers_refuse_bad_calls():
     c = ops.PagedCache(4, 16, 2, 64, device="cpu")
     x, t, n = torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
@@ -169,20 +164,48 @@ def test_wrappers_refuse_bad_calls():
         c.append(x, x, t, n)
     with pytest.raises(ValueError, match="HIP device"):
         ops.paged_attention(x, c, t, n)
-    c.k = c.k.as_subclass(Cuda)
-    with pytest.raises(ValueError, match="lengths is missing"):
-        c.append(x, x, t, None)
-    with pytest.raises(ValueError, match="lengths is missing"):
-        ops.paged_attention(x, c, t, None)
-    bad = [
+    # what the compiled module refuses before any launch, here of a cache on the host
+    M = gm.torch_lib()
+
+    def attend(q=x, table=t, lengths=n, offsets=None, slopes=None, out=None, window=0, scale=0.1):
+        return M.attention(c._address, c.k, q, table, lengths, offsets, window, 0.0, slopes, scale, out, 0)
+
+    def append(q=x, table=t, lengths=n, offsets=None, v=None, cos=None, sin=None, queries=None, q_out=None):
+        return M.append(c._address, c.k, q, q if v is None else v, table, lengths, offsets, cos, sin, queries, q_out, 0)
+
+    for kw, message in [
         (dict(q=x[:, 0]), "without"), (dict(offsets=torch.zeros(3, dtype=torch.int32)), "with offsets"),
-        (dict(table=t.long()), "int32"), (dict(table=t[0]), "table must"), (dict(table=torch.zeros(3, 2, dtype=torch.int32).t()), "table must"),
-        (dict(table=t[:1]), "sequences"), (dict(lengths=n.long()), "lengths must"), (dict(lengths=n[:1]), "lengths must"),
-        (dict(q=x[0], offsets=n), "offsets must"),
-    ]
-    for kw, message in bad:
-        a = {**dict(q=x, table=t, lengths=n, offsets=None), **kw}
+        (dict(table=t.long()), "int32"), (dict(table=t[0]), "table must"),
+        (dict(table=torch.zeros(3, 2, dtype=torch.int32).t()), "table must"), (dict(table=t[:1]), "sequences"),
+        (dict(lengths=n.long()), "lengths must"), (dict(lengths=n[:1]), "lengths must"),
+        (dict(lengths=torch.zeros(4, dtype=torch.int32)[::2]), "lengths must"), (dict(lengths=None), "lengths is missing"),
+        (dict(q=x[0], offsets=n), "offsets must"), (dict(q=x.half()), "must be BFloat16"),
+        (dict(q=x[..., :32]), "must be BFloat16 of shape"), (dict(q=torch.zeros(2, 1, 64, 2, dtype=torch.bfloat16).transpose(2, 3)), "channels"),
+    ]:
+        for call in (attend, append):
+            with pytest.raises(ValueError, match=message):
+                call(**kw)
+    with pytest.raises(ValueError, match="12 arguments"):
+        M.append(1)
+    with pytest.raises(TypeError, match="must be a tensor"):
+        attend(q=[1.0])
+    with pytest.raises(TypeError):
+        attend(window=1.5)
+    with pytest.raises(TypeError):
+        attend(scale="x")
+    for kw, message in [(dict(out=x.half()), "out must"), (dict(out=x[0]), "out must"), (dict(slopes=n), "slopes must"),
+                        (dict(slopes=torch.zeros(3)), "slopes must")]:
         with pytest.raises(ValueError, match=message):
-            ops.paged_attention(a["q"], c, a["table"], a["lengths"], offsets=a["offsets"])
+            attend(**kw)
+    r = torch.zeros(48, 32)
+    for kw, message in [
+        (dict(v=x.half()), "v must"), (dict(v=x[..., :1, :]), "v must"), (dict(cos=r[0], sin=r), "cos must be"),
+        (dict(cos=r, sin=r[1:]), "sin must"), (dict(cos=r.double(), sin=r), "cos must"), (dict(cos=r.t(), sin=r), "cos must"),
+        (dict(queries=x[0]), "dimensions"), (dict(queries=x.half()), "q must"), (dict(queries=x[:1]), "q must"),
+        (dict(q_out=x), "q_out needs q"), (dict(queries=x, q_out=x[:, :0]), "q_out must"),
+    ]:
         with pytest.raises(ValueError, match=message):
-            c.append(a["q"], a["q"], a["table"], a["lengths"], offsets=a["offsets"])
+            append(**kw)
+    # codes of the C entry come back as numbers: a window below 0 and one past an int
+    assert attend(window=-1) == gm.GM_E_INVAL and attend(window=1 << 40) == gm.GM_E_INVAL
+    assert append(cos=r[:40], sin=r[:40]) == gm.GM_E_INVAL and b"every position" in gm.lib().gm_last_error()
