@@ -18,6 +18,21 @@ __device__ __forceinline__ int32_t const_load(const int32_t* p) {
   return *(cptr)reinterpret_cast<uintptr_t>(p);
 }
 
+// 16 bytes of LDS, as lds_read_tr16 reads them: the compiler makes such a read wait for
+// every copy into LDS in flight, and each before the next.  lgkm_wait16() must precede any use.
+template <int OFF>
+__device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {
+  u32x4 v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "i"(OFF) : "memory");
+  return v;
+}
+// Wait until at most N LDS reads are outstanding, then tie two values to the wait.
+template <int N>
+__device__ __forceinline__ void lgkm_wait16(u32x4 (&v)[2]) {
+  asm volatile("s_waitcnt lgkmcnt(%0)" ::"i"(N) : "memory");
+  asm volatile("" : "+v"(v[0]), "+v"(v[1]));
+}
+
 // One sequence of an attention call: its query rows, n tokens from row row0 of the packed
 // rows, its keys [lo, kend) that any of them may see, and the position p0 of the first.
 struct PagedSeq {

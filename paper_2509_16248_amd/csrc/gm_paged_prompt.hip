@@ -126,10 +126,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
   constexpr int RPI = 64 / CPR;               // key rows per 1 KB copy instruction
   constexpr int LPW = KB / RPI / NW;          // copy instructions per wavefront, tile and operand
   constexpr int TILE = KB * HD;
-  __shared__ __attribute__((aligned(1024))) T sK0[TILE];
-  __shared__ __attribute__((aligned(1024))) T sK1[TILE];
-  __shared__ __attribute__((aligned(1024))) T sV0[TILE];
-  __shared__ __attribute__((aligned(1024))) T sV1[TILE];
+  __shared__ __attribute__((aligned(1024))) T lds[4 * TILE];   // K of two stages, V of two
 
   // heads fastest: the blocks of a key head come to one XCD where the heads are a
   // multiple of 8
@@ -177,19 +174,41 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
   };
   // swizzles: chunk e of key row r sits at chunk position e ^ f(r) (k_flash)
   const int cr = lane / CPR, cpos = lane % CPR;
+  // a lane's bytes from the first row of a copy instruction: of K for each, of V the same for all
+  uint32_t koff[LPW];
+#pragma unroll
+  for (int j = 0; j < LPW; ++j)
+    koff[j] = 2 * (cr * HD + 8 * (cpos ^ (((wave * LPW + j) * RPI + cr) / RPL % CPR)));
+  const uint32_t voff = 2 * (cr * HD + 8 * (cpos ^ 4 * (cr / RPL % (CPR / 4))));
+  static_assert(RPI / RPL % (CPR / 4) == 0, "V's swizzle is the same for every copy instruction");
+  const int64_t page_bytes = static_cast<int64_t>(c.heads) * c.page_size * HD * 2;
+  const int64_t head_bytes = static_cast<int64_t>(kvh) * c.page_size * HD * 2;
   // the tile at kb, whose entries are ids; its keys that are in no hole are returned
   auto issue = [&](int kb, int ids, T* dk, T* dv) {
     const bool ok = static_cast<unsigned>(ids) < static_cast<unsigned>(c.pages);
     const int id = ok ? ids : 0;
+    const int row0 = wave * LPW * RPI;
+    if (kb + KB <= kend) {
 #pragma unroll
-    for (int j = 0; j < LPW; ++j) {
-      const int row = (wave * LPW + j) * RPI;
-      const int first = kb + row < (last_key & ~(RPI - 1)) ? kb + row : last_key & ~(RPI - 1);
-      const int64_t at = paged_base(c, __builtin_amdgcn_readlane(id, first - kb), kvh) + (first & in_page) * HD;
-      const int in = first + cr < last_key ? cr : last_key - first;
-      const int fk = ((row + cr) / RPL) % CPR, fv = 4 * (((row + cr) / RPL) % (CPR / 4));
-      dma16(static_cast<const T*>(c.k) + at + in * HD + 8 * (cpos ^ fk), dk + row * HD);
-      dma16(static_cast<const T*>(c.v) + at + in * HD + 8 * (cpos ^ fv), dv + row * HD);
+      for (int j = 0; j < LPW; ++j) {
+        const int row = row0 + j * RPI;
+        const int64_t at = __builtin_amdgcn_readlane(id, row) * page_bytes + head_bytes +
+                           static_cast<int64_t>(((kb + row) & in_page) * HD * 2);
+        dma16(static_cast<const char*>(c.k) + at + koff[j], dk + row * HD);
+        dma16(static_cast<const char*>(c.v) + at + voff, dv + row * HD);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < LPW; ++j) {
+        const int row = row0 + j * RPI;
+        const int first = kb + row < (last_key & ~(RPI - 1)) ? kb + row : last_key & ~(RPI - 1);
+        const int64_t at = __builtin_amdgcn_readlane(id, first - kb) * page_bytes + head_bytes +
+                           static_cast<int64_t>((first & in_page) * HD * 2);
+        // (a row past the last repeats it)
+        const int back = first + cr < last_key ? 0 : (first + cr - last_key) * HD * 2;
+        dma16(static_cast<const char*>(c.k) + at + (static_cast<int>(koff[j]) - back), dk + row * HD);
+        dma16(static_cast<const char*>(c.v) + at + (static_cast<int>(voff) - back), dv + row * HD);
+      }
     }
     return __ballot(ok);
   };
@@ -199,21 +218,23 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
   const int vswz4 = (vrow / RPL) % (CPR / 4);
   const int vsub = 2 * (g & 1) + (q4 >> 1);
   const int vin = 4 * (q4 & 1);
-  uint32_t vaddr[CB];
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_vptr)lds));
+  uint32_t kaddr[KS], vaddr[CB];              // in stage 0
 #pragma unroll
-  for (int e = 0; e < CB; ++e) vaddr[e] = 2 * (vrow * HD + 8 * (4 * (e ^ vswz4) + vsub) + vin);
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = lds0 + 2 * (l32 * HD + 8 * ((2 * ks + h2) ^ kswz));
+#pragma unroll
+  for (int e = 0; e < CB; ++e) vaddr[e] = lds0 + 2 * (2 * TILE + vrow * HD + 8 * (4 * (e ^ vswz4) + vsub) + vin);
 
   unsigned long long there[2] = {0, 0};       // keys of the stages' tiles that are in no hole
   int ids = 0;                                // entries of the tile after the next
   // one key tile from stage BUF (the other stage receives the next one)
   auto tile = [&](auto BUF, int kb) {
-    constexpr int buf = decltype(BUF)::value;
-    T* sk = buf ? sK1 : sK0;
-    T* sv = buf ? sV1 : sV0;
+    constexpr int buf = decltype(BUF)::value, STAGE = 2 * buf * TILE;   // bytes of it
+    T* other = lds + (buf ^ 1) * TILE;
     wait_vmcnt0();                            // this wavefront's copies of the tile landed
     __syncthreads();
     if (kb + KB < kend) {
-      there[buf ^ 1] = issue(kb + KB, ids, buf ? sK0 : sK1, buf ? sV0 : sV1);
+      there[buf ^ 1] = issue(kb + KB, ids, other, other + 2 * TILE);
       ids = entries(kb + 2 * KB);
     }
     // no key of the tile is seen by this wavefront's rows
@@ -225,13 +246,29 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sacc[kk][i] = 0.f;
+    // (the K operands of two k steps on their way while one multiplies)
+    u32x4 kf[3][2];
+    auto kread = [&](int ks) {
+      kf[ks % 3][0] = lds_read16<STAGE>(kaddr[ks]);
+      kf[ks % 3][1] = lds_read16<STAGE + 64 * HD>(kaddr[ks]);
+    };
+    auto kmul = [&](int ks) {
+      sacc[0] = Mfma32A<T>::run(__builtin_bit_cast(vec, kf[ks % 3][0]), qf[ks], sacc[0]);
+      sacc[1] = Mfma32A<T>::run(__builtin_bit_cast(vec, kf[ks % 3][1]), qf[ks], sacc[1]);
+    };
+    kread(0);
+    kread(1);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        const vec kf = *reinterpret_cast<const vec*>(sk + (32 * kk + l32) * HD + 8 * ((2 * ks + h2) ^ kswz));
-        sacc[kk] = Mfma32A<T>::run(kf, qf[ks], sacc[kk]);
+      if (ks + 2 < KS) {
+        kread(ks + 2);
+        lgkm_wait16<4>(kf[ks % 3]);
+      } else if (ks + 1 < KS) {
+        lgkm_wait16<2>(kf[ks % 3]);
+      } else {
+        lgkm_wait16<0>(kf[ks % 3]);
       }
+      kmul(ks);
     }
     // ---- capped scores, in log2 units
     if constexpr (CAP) {
@@ -282,8 +319,28 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
       mrun = mnew;
     }
     const float msub = mrun == -INFINITY ? 0.f : mrun - kUp;
-    // ---- probabilities, their sum, and P^T as 16-bit B operands
+    // ---- O^T += V^T P^T: four 16-key steps; the V^T operands of step k2 + 1 are read
+    // while step k2 multiplies, those of the first while the probabilities are computed
     vec pb[4];
+    u32x2 vf[2][CB][2];
+    auto vread = [&](auto K2, u32x2 (&dst)[CB][2]) {
+      constexpr int k2 = decltype(K2)::value;
+#pragma unroll
+      for (int e = 0; e < CB; ++e) {
+        dst[e][0] = lds_read_tr16<STAGE + (16 * k2) * HD * 2>(vaddr[e]);
+        dst[e][1] = lds_read_tr16<STAGE + (16 * k2 + 8) * HD * 2>(vaddr[e]);
+      }
+    };
+    auto vmul = [&](int k2, u32x2 (&src)[CB][2]) {
+#pragma unroll
+      for (int e = 0; e < CB; ++e) {
+        u32x4 v;
+        v[0] = src[e][0][0]; v[1] = src[e][0][1]; v[2] = src[e][1][0]; v[3] = src[e][1][1];
+        oacc[e] = Mfma32A<T>::run(__builtin_bit_cast(vec, v), pb[k2], oacc[e]);
+      }
+    };
+    vread(std::integral_constant<int, 0>(), vf[0]);
+    // ---- probabilities, their sum, and P^T as 16-bit B operands
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
@@ -300,27 +357,6 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
         pb[2 * kk + hf] = __builtin_bit_cast(vec, v);
       }
     }
-    // ---- O^T += V^T P^T: four 16-key steps; the V^T operands of step
-    // k2 + 1 are read while step k2 multiplies
-    const uint32_t vb = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_vptr)sv));
-    u32x2 vf[2][CB][2];
-    auto vread = [&](auto K2, u32x2 (&dst)[CB][2]) {
-      constexpr int k2 = decltype(K2)::value;
-#pragma unroll
-      for (int e = 0; e < CB; ++e) {
-        dst[e][0] = lds_read_tr16<(16 * k2) * HD * 2>(vb + vaddr[e]);
-        dst[e][1] = lds_read_tr16<(16 * k2 + 8) * HD * 2>(vb + vaddr[e]);
-      }
-    };
-    auto vmul = [&](int k2, u32x2 (&src)[CB][2]) {
-#pragma unroll
-      for (int e = 0; e < CB; ++e) {
-        u32x4 v;
-        v[0] = src[e][0][0]; v[1] = src[e][0][1]; v[2] = src[e][1][0]; v[3] = src[e][1][1];
-        oacc[e] = Mfma32A<T>::run(__builtin_bit_cast(vec, v), pb[k2], oacc[e]);
-      }
-    };
-    vread(std::integral_constant<int, 0>(), vf[0]);
     vread(std::integral_constant<int, 1>(), vf[1]);
     lgkm_wait<2 * CB>(&vf[0][0][0], 2 * CB);
     vmul(0, vf[0]);
@@ -334,7 +370,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
     vmul(3, vf[1]);
   };
   if (w.k0 < kend) {
-    there[0] = issue(w.k0, entries(w.k0), sK0, sV0);
+    there[0] = issue(w.k0, entries(w.k0), lds, lds + 2 * TILE);
     ids = entries(w.k0 + KB);
     for (int kb = w.k0;; kb += 2 * KB) {
       tile(std::integral_constant<int, 0>(), kb);
