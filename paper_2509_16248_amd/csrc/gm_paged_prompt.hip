@@ -101,6 +101,22 @@ __device__ __forceinline__ float* prompt_part(const gm_paged_attention_args& a, 
   return static_cast<float*>(a.workspace) + (w.item * p.nsplit + split) * kRows * (HD + 2);
 }
 
+// One, two or four instructions of 1 KB into LDS, one after the other there and, but for a
+// lane's own bytes off[j], in memory.
+__device__ __forceinline__ void copy_rows(const char* g, const uint32_t (&off)[1], void* lds) {
+  __builtin_amdgcn_global_load_lds(g + off[0], (lds_vptr)lds, 16, 0, 0);
+}
+__device__ __forceinline__ void copy_rows(const char* g, const uint32_t (&off)[2], void* lds) {
+  __builtin_amdgcn_global_load_lds(g + off[0], (lds_vptr)lds, 16, 0, 0);
+  __builtin_amdgcn_global_load_lds(g + off[1], (lds_vptr)lds, 16, 1024, 0);
+}
+__device__ __forceinline__ void copy_rows(const char* g, const uint32_t (&off)[4], void* lds) {
+  __builtin_amdgcn_global_load_lds(g + off[0], (lds_vptr)lds, 16, 0, 0);
+  __builtin_amdgcn_global_load_lds(g + off[1], (lds_vptr)lds, 16, 1024, 0);
+  __builtin_amdgcn_global_load_lds(g + off[2], (lds_vptr)lds, 16, 2048, 0);
+  __builtin_amdgcn_global_load_lds(g + off[3], (lds_vptr)lds, 16, 3072, 0);
+}
+
 constexpr int paged_prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 : 4; }
 
 // Workgroup = 128 query rows of one (sequence, key head), as k_prompt_flash
@@ -174,40 +190,37 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
   };
   // swizzles: chunk e of key row r sits at chunk position e ^ f(r) (k_flash)
   const int cr = lane / CPR, cpos = lane % CPR;
-  // a lane's bytes from the first row of a copy instruction: of K for each, of V the same for all
+  // A wavefront's rows of a tile, 16 of them, lie in one page.  A lane's bytes from the first
+  // row of a copy instruction: of K for each, of V the same for all.
+  static_assert(LPW * RPI == 16 && RPI * HD * 2 == 1024, "a wavefront copies 16 rows, 1 KB at a time");
+  static_assert(RPI / RPL % (CPR / 4) == 0, "V's swizzle is the same for every copy instruction");
   uint32_t koff[LPW];
 #pragma unroll
   for (int j = 0; j < LPW; ++j)
     koff[j] = 2 * (cr * HD + 8 * (cpos ^ (((wave * LPW + j) * RPI + cr) / RPL % CPR)));
   const uint32_t voff = 2 * (cr * HD + 8 * (cpos ^ 4 * (cr / RPL % (CPR / 4))));
-  static_assert(RPI / RPL % (CPR / 4) == 0, "V's swizzle is the same for every copy instruction");
   const int64_t page_bytes = static_cast<int64_t>(c.heads) * c.page_size * HD * 2;
-  const int64_t head_bytes = static_cast<int64_t>(kvh) * c.page_size * HD * 2;
+  const char* kbase = static_cast<const char*>(c.k) + static_cast<int64_t>(kvh) * c.page_size * HD * 2;
+  const char* vbase = static_cast<const char*>(c.v) + static_cast<int64_t>(kvh) * c.page_size * HD * 2;
   // the tile at kb, whose entries are ids; its keys that are in no hole are returned
-  auto issue = [&](int kb, int ids, T* dk, T* dv) {
+  auto issue = [&](int kb, int ids, T* dst) {
     const bool ok = static_cast<unsigned>(ids) < static_cast<unsigned>(c.pages);
-    const int id = ok ? ids : 0;
-    const int row0 = wave * LPW * RPI;
+    const int id = ok ? ids : 0, row = wave * 16;
+    T *dk = dst + row * HD, *dv = dk + 2 * TILE;
     if (kb + KB <= kend) {
-#pragma unroll
-      for (int j = 0; j < LPW; ++j) {
-        const int row = row0 + j * RPI;
-        const int64_t at = __builtin_amdgcn_readlane(id, row) * page_bytes + head_bytes +
-                           static_cast<int64_t>(((kb + row) & in_page) * HD * 2);
-        dma16(static_cast<const char*>(c.k) + at + koff[j], dk + row * HD);
-        dma16(static_cast<const char*>(c.v) + at + voff, dv + row * HD);
-      }
+      const int64_t at = __builtin_amdgcn_readlane(id, row) * page_bytes + ((kb + row) & in_page) * (HD * 2);
+      copy_rows(kbase + at, koff, dk);
+      const uint32_t same[LPW] = {};
+      copy_rows(vbase + at + voff, same, dv);
     } else {
+      // (rows past the last key repeat it; a wavefront's rows that all lie past it those before)
+      const int first = kb + row < (last_key & ~15) ? kb + row : last_key & ~15;
+      const int64_t at = __builtin_amdgcn_readlane(id, first - kb) * page_bytes + (first & in_page) * (HD * 2);
 #pragma unroll
       for (int j = 0; j < LPW; ++j) {
-        const int row = row0 + j * RPI;
-        const int first = kb + row < (last_key & ~(RPI - 1)) ? kb + row : last_key & ~(RPI - 1);
-        const int64_t at = __builtin_amdgcn_readlane(id, first - kb) * page_bytes + head_bytes +
-                           static_cast<int64_t>((first & in_page) * HD * 2);
-        // (a row past the last repeats it)
-        const int back = first + cr < last_key ? 0 : (first + cr - last_key) * HD * 2;
-        dma16(static_cast<const char*>(c.k) + at + (static_cast<int>(koff[j]) - back), dk + row * HD);
-        dma16(static_cast<const char*>(c.v) + at + (static_cast<int>(voff) - back), dv + row * HD);
+        const int past = first + j * RPI + cr - last_key, back = past > 0 ? past * HD * 2 : 0;
+        dma16(kbase + at + (static_cast<int>(koff[j]) + j * 1024 - back), dk + j * RPI * HD);
+        dma16(vbase + at + (static_cast<int>(voff) + j * 1024 - back), dv + j * RPI * HD);
       }
     }
     return __ballot(ok);
@@ -234,7 +247,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
     wait_vmcnt0();                            // this wavefront's copies of the tile landed
     __syncthreads();
     if (kb + KB < kend) {
-      there[buf ^ 1] = issue(kb + KB, ids, other, other + 2 * TILE);
+      there[buf ^ 1] = issue(kb + KB, ids, other);
       ids = entries(kb + 2 * KB);
     }
     // no key of the tile is seen by this wavefront's rows
@@ -370,7 +383,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
     vmul(3, vf[1]);
   };
   if (w.k0 < kend) {
-    there[0] = issue(w.k0, entries(w.k0), lds, lds + 2 * TILE);
+    there[0] = issue(w.k0, entries(w.k0), lds);
     ids = entries(w.k0 + KB);
     for (int kb = w.k0;; kb += 2 * KB) {
       tile(std::integral_constant<int, 0>(), kb);
