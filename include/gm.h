@@ -547,7 +547,7 @@ typedef struct gm_paged_cache {
  * [B, n, heads, head_dim], n tokens a sequence; or, with offsets (int32 [B + 1],
  * ascending), packed: [n, heads, head_dim] with n rows in all (a gm_tensor whose
  * `batch` is not looked at), rows offsets[b] .. offsets[b + 1] - 1 being sequence
- * b's and rows of no sequence neither read nor written.
+ * b's; what stands in rows of no sequence does not matter, and it is left there.
  *  lengths  int32 [B]: tokens of each sequence, the new ones included: token i
  *           of n_b new ones is at position lengths[b] - n_b + i
  *  table    int32 [B, width], rows table_stride elements apart: position p of

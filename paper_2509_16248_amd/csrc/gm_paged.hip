@@ -37,33 +37,43 @@ template <typename T> struct Half8 {       // 8 channels
 
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm_paged_cache c) {
-  constexpr int LPR = HD / 16, U = 4;
+  constexpr int LPR = HD / 16, U = 4, STEP = 256 / LPR;
   const gm_paged_rows& r = a.rows;
+  const int row = blockIdx.x, nq = a.n_q_heads, heads = nq + 2 * c.heads;
+  const int ch = threadIdx.x % LPR;
+  const bool turns = ch < a.rot / 16;
+  // packed rows are one sequence as far as their tensors go
+  const int first = r.offsets ? 0 : row / r.n, i = r.offsets ? row : row - first * r.n;
+  Half8<T> lo[U], hi[U];
+  // of pairs that turn, and of 16 channels in a row (values: from the head's start)
+  auto from = [&](int h) { return turns && h < nq + c.heads ? 8 * ch : 16 * ch; };
+  auto to = [&](int h) { return turns && h < nq + c.heads ? 8 * ch + a.rot / 2 : 16 * ch + 8; };
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * STEP;
+      if (h >= heads) break;
+      const gm_tensor& t = h < nq ? a.q : h < nq + c.heads ? a.k : a.v;
+      const int hh = h < nq ? h : h < nq + c.heads ? h - nq : h - nq - c.heads;
+      const T* x = static_cast<const T*>(t.p) + first * t.batch + i * t.token + hh * t.head;
+      lo[u].load(x + from(h));
+      hi[u].load(x + to(h));
+    }
+  };
+  const int h1 = threadIdx.x / LPR;
+  fetch(h1);                                 // (on their way while the place is looked up)
   // ---- whose token this is, and its position
-  int b, i, row = blockIdx.x;
-  int64_t pos;
+  const int b = r.offsets ? paged_sequence_of(r, row) : first;
+  if (b >= r.B) return;
+  int end = r.n, before = i;                 // of the sequence's rows, and the token's place in them
   if (r.offsets) {
-    b = paged_sequence_of(r, row);
-    if (b >= r.B) return;
-    const int o0 = const_load(r.offsets + b), end = const_load(r.offsets + b + 1), o1 = end < r.n ? end : r.n;
-    if (row < o0) return;
-    i = row;
-    pos = static_cast<int64_t>(const_load(r.lengths + b)) - o1 + row;
-  } else {
-    b = row / r.n;
-    i = row - b * r.n;
-    pos = static_cast<int64_t>(const_load(r.lengths + b)) - r.n + i;
+    const int o1 = const_load(r.offsets + b + 1);
+    if (row < const_load(r.offsets + b)) return;
+    end = o1 < r.n ? o1 : r.n;
   }
+  const int64_t pos = static_cast<int64_t>(const_load(r.lengths + b)) - end + before;
   const bool inside = pos >= 0 && pos < static_cast<int64_t>(r.width) * c.page_size;
   const int p = inside ? static_cast<int>(pos) : 0, lg = 31 - __builtin_clz(c.page_size);
-  const int page = const_load(r.table + b * r.table_stride + (p >> lg));
-  const bool stored = inside && page >= 0 && page < c.pages;
-  const int64_t slot = paged_base(c, stored ? page : 0, 0) + (p & (c.page_size - 1)) * HD;
-  const int64_t head_step = static_cast<int64_t>(c.page_size) * HD;
-  const int64_t first = r.offsets ? 0 : b;
-
-  const int ch = threadIdx.x % LPR, turned = a.rot / 16;
-  const bool turns = ch < turned;
   float cosv[8], sinv[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -80,27 +90,15 @@ __global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm
 #pragma unroll
     for (int j = 0; j < 8; ++j) sinv[j] = x.get(j);
   }
-  const int nq = a.n_q_heads, heads = nq + 2 * c.heads;
-  for (int h0 = threadIdx.x / LPR; h0 < heads; h0 += U * (256 / LPR)) {
-    Half8<T> lo[U], hi[U];
-    int from[U], to[U];                      // channels of the two halves
+  const int page = const_load(r.table + b * r.table_stride + (p >> lg));
+  const bool stored = inside && page >= 0 && page < c.pages;
+  const int64_t slot = paged_base(c, stored ? page : 0, 0) + (p & (c.page_size - 1)) * HD;
+  const int64_t head_step = static_cast<int64_t>(c.page_size) * HD;
+  for (int h0 = h1; h0 < heads; h0 += U * STEP) {
+    if (h0 != h1) fetch(h0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * (256 / LPR);
-      const bool turn = turns && h < nq + c.heads;
-      // of pairs that turn, and of 16 channels in a row (values: from the head's start)
-      from[u] = turn ? 8 * ch : 16 * ch;
-      to[u] = turn ? 8 * ch + a.rot / 2 : 16 * ch + 8;
-      if (h >= heads) continue;
-      const gm_tensor& t = h < nq ? a.q : h < nq + c.heads ? a.k : a.v;
-      const int hh = h < nq ? h : h < nq + c.heads ? h - nq : h - nq - c.heads;
-      const T* x = static_cast<const T*>(t.p) + first * t.batch + i * t.token + hh * t.head;
-      lo[u].load(x + from[u]);
-      hi[u].load(x + to[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * (256 / LPR);
+      const int h = h0 + u * STEP;
       if (h >= heads) break;
       if (turns && h < nq + c.heads) {
 #pragma unroll
@@ -122,8 +120,8 @@ __global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm
         const bool key = h < nq + c.heads;
         out = static_cast<T*>(key ? c.k : c.v) + slot + (h - nq - (key ? 0 : c.heads)) * head_step;
       }
-      lo[u].store(out + from[u]);
-      hi[u].store(out + to[u]);
+      lo[u].store(out + from(h));
+      hi[u].store(out + to(h));
     }
   }
 }

@@ -41,9 +41,14 @@ __device__ __forceinline__ PromptPlace prompt_place(const gm_paged_attention_arg
   w.item = static_cast<long long>(block) * c.heads + kvh;
   int qb;                                // counted from the first row
   if (p.blocks) {
-    // (later tokens, which see more keys, first; sequences in turn)
-    const int x = block / a.rows.B;
+    // later tokens, which see more keys, first; sequences in turn.  Of up to 512 items, which run
+    // at once, the second 256 with their blocks the other way round, so that the two
+    // workgroups of a CU are a long and a short one (2048 tokens, 32 heads of 128: 53.6 -> 50.7
+    // us; more items run one after the other, and lose 1 to 3%).
+    const int pairs = a.rows.B * c.heads, slot = (block * c.heads) / 256;
+    int x = block / a.rows.B;
     w.b = block - x * a.rows.B;
+    if (256 % pairs == 0 && slot == 1 && p.most * c.heads == 512) x = 3 * (256 / pairs) - 1 - x;
     qb = p.blocks - 1 - x;
     w.s = paged_seq(a, c, w.b);
   } else {
