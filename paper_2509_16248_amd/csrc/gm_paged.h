@@ -43,12 +43,12 @@ __device__ __forceinline__ PagedSeq paged_seq(const gm_paged_attention_args& a, 
   s.row0 = 0;
   s.n = a.rows.n;
   if (a.rows.offsets) {
-    const int o0 = a.rows.offsets[b], o1 = a.rows.offsets[b + 1];
+    const int o0 = const_load(a.rows.offsets + b), o1 = const_load(a.rows.offsets + b + 1);
     s.row0 = o0 < 0 ? 0 : o0 < a.rows.n ? o0 : a.rows.n;
     s.n = (o1 < a.rows.n ? o1 : a.rows.n) - s.row0;
     s.n = s.n > 0 ? s.n : 0;
   }
-  const int len = a.rows.lengths[b], cap = a.rows.width * c.page_size;
+  const int len = const_load(a.rows.lengths + b), cap = a.rows.width * c.page_size;
   s.kend = len < 0 ? 0 : len < cap ? len : cap;
   s.p0 = (len < 0 ? 0 : len) - s.n;
   s.lo = a.window > 0 && s.p0 - a.window + 1 > 0 ? s.p0 - a.window + 1 : 0;

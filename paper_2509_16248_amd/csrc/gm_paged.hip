@@ -293,26 +293,6 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
   // ---- rows [blk * R, ...) of key head kvh over the keys [k0, k1); part: where a cut
   // item's rows go
   auto work = [&](int b, const PagedSeq& s, int kvh, int blk, int k0, int k1, float* part) {
-    const int rows = s.n * plan.G, r0 = blk * R;
-    const int rlast = r0 + R < rows ? r0 + R - 1 : rows - 1;
-    const int qmin = s.p0 + r0 / plan.G, qmax = s.p0 + rlast / plan.G;
-    k1 = k1 < qmax + 1 ? k1 : qmax + 1;
-    k1 = k1 < s.kend ? k1 : s.kend;
-    if (a.window > 0 && k0 < qmin - a.window + 1) k0 = (qmin - a.window + 1) & ~(KB - 1);
-    int qpos[NSET], qlow[NSET];
-    float slope2[NSET];
-    u32x4 qf[NSET][KC];
-#pragma unroll
-    for (int x = 0; x < NSET; ++x) {
-      const int r = r0 + 16 * x + n <= rlast ? r0 + 16 * x + n : r0;   // (columns past the last repeat the first)
-      const int i = r / plan.G, h = kvh * plan.G + r - i * plan.G;
-      qpos[x] = s.p0 + i;
-      qlow[x] = a.window > 0 ? qpos[x] - a.window : -1;
-      slope2[x] = a.scores.slopes ? a.scores.slopes[h] * kPagedLog2e : 0.f;
-      const char* q = reinterpret_cast<const char*>(paged_row_at<const T>(a.q, a.rows, b, s.row0, i, h)) + 16 * g;
-#pragma unroll
-      for (int e = 0; e < KC; ++e) qf[x][e] = *reinterpret_cast<const u32x4*>(q + 64 * e);
-    }
     const int32_t* table = a.rows.table + b * a.rows.table_stride;
     const int last_page = a.rows.width - 1;
     auto page_of = [&](int key) {
@@ -347,6 +327,30 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
         for (int r = 0; r < 4; ++r) load_row<VB>(base + voff + r * RB, t.v[4 * u + r]);
       }
     };
+    // (of the first tile, if the keys begin at 0: looked up together with the length)
+    const bool known = plan.wgs == 0 && a.window == 0;
+    Ids i0;
+    if (known) i0 = ids_of(KB * wave);
+    const int rows = s.n * plan.G, r0 = blk * R;
+    const int rlast = r0 + R < rows ? r0 + R - 1 : rows - 1;
+    const int qmin = s.p0 + r0 / plan.G, qmax = s.p0 + rlast / plan.G;
+    k1 = k1 < qmax + 1 ? k1 : qmax + 1;
+    k1 = k1 < s.kend ? k1 : s.kend;
+    if (a.window > 0 && k0 < qmin - a.window + 1) k0 = (qmin - a.window + 1) & ~(KB - 1);
+    int qpos[NSET], qlow[NSET];
+    float slope2[NSET];
+    u32x4 qf[NSET][KC];
+#pragma unroll
+    for (int x = 0; x < NSET; ++x) {
+      const int r = r0 + 16 * x + n <= rlast ? r0 + 16 * x + n : r0;   // (columns past the last repeat the first)
+      const int i = r / plan.G, h = kvh * plan.G + r - i * plan.G;
+      qpos[x] = s.p0 + i;
+      qlow[x] = a.window > 0 ? qpos[x] - a.window : -1;
+      slope2[x] = a.scores.slopes ? a.scores.slopes[h] * kPagedLog2e : 0.f;
+      const char* q = reinterpret_cast<const char*>(paged_row_at<const T>(a.q, a.rows, b, s.row0, i, h)) + 16 * g;
+#pragma unroll
+      for (int e = 0; e < KC; ++e) qf[x][e] = *reinterpret_cast<const u32x4*>(q + 64 * e);
+    }
     float m[NSET], l[NSET];
     f32x4 o[NSET][NI];
 #pragma unroll
@@ -447,14 +451,16 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
     };
     float sc[NSET][NS];
     int kb = k0 + KB * wave;
+    if (!known) i0 = ids_of(kb);
+    Tile t0;
+    if (kb < k1) {
+      fetch_k(kb, i0, t0);
+      fetch_v(kb, i0, t0);
+    }
     if constexpr (NSET == 1) {
       // two tiles in turn, one being worked on while the other arrives
-      Tile t0, t1;
-      Ids i0 = ids_of(kb), i1 = ids_of(kb + UNIT);
-      if (kb < k1) {
-        fetch_k(kb, i0, t0);
-        fetch_v(kb, i0, t0);
-      }
+      Tile t1;
+      Ids i1 = ids_of(kb + UNIT);
       while (kb < k1) {
         if (kb + UNIT < k1) {
           fetch_k(kb + UNIT, i1, t1);
@@ -478,18 +484,13 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
       }
     } else {
       // one tile, its parts loaded anew as soon as they have been used
-      Tile t;
-      Ids i0 = ids_of(kb), i1 = ids_of(kb + UNIT);
-      if (kb < k1) {
-        fetch_k(kb, i0, t);
-        fetch_v(kb, i0, t);
-      }
+      Ids i1 = ids_of(kb + UNIT);
       for (; kb < k1; kb += UNIT) {
         const Ids i2 = ids_of(kb + 2 * UNIT);
-        scores(kb, t, sc);
-        if (kb + UNIT < k1) fetch_k(kb + UNIT, i1, t);
-        values(kb, i0, t, sc);
-        if (kb + UNIT < k1) fetch_v(kb + UNIT, i1, t);
+        scores(kb, t0, sc);
+        if (kb + UNIT < k1) fetch_k(kb + UNIT, i1, t0);
+        values(kb, i0, t0, sc);
+        if (kb + UNIT < k1) fetch_v(kb + UNIT, i1, t0);
         i0 = i1;
         i1 = i2;
       }
