@@ -178,6 +178,6 @@ void by_paged_cache(const gm_paged_cache& c, F f) {
 // gm_paged_prompt.hip: 16-bit chunks of many rows.  Sequences of at most `few` query rows
 // per key head are left to the rows kernel (0: none are).
 void launch_paged_prompt(const gm_paged_attention_args& a, int few, hipStream_t s);
-uint64_t paged_prompt_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, bool packed);
+uint64_t paged_prompt_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, int few, bool packed);
 
 }  // namespace gm

@@ -142,7 +142,7 @@ struct PagedPlan {
   int few;       // sequences of more rows than this are another kernel's (0: none are)
   int wgs;       // workgroups that share all tiles; 0: a workgroup an item
   int items;     // items there are at the most
-  int joined;    // rows of a (sequence, key head) that the join looks at; 0: by token and head
+  int joined;    // rows of a block at the most
 };
 
 constexpr int kMostParts = 64;     // workgroups that share an item
@@ -168,12 +168,16 @@ struct PagedFound {
   int b;                       // its sequence; -1: none
   unsigned items, tiles;       // those of the sequences before
   unsigned all_tiles;
+  unsigned at;                 // the item, or the tile
   int per;                     // tiles a workgroup takes
 };
-// By one wavefront: the sequence that item or (by_tile) workgroup `x` falls into.
-template <int R, int UNIT>
+// By one wavefront: the sequence that item x (FIND_ITEM), or workgroup x's first or last
+// tile falls into.
+enum { FIND_ITEM, FIND_FIRST, FIND_LAST };
+template <int R, int UNIT, int WHAT>
 __device__ __forceinline__ PagedFound paged_find(const gm_paged_attention_args& a, const gm_paged_cache& c,
-                                                 const PagedPlan& p, unsigned x, bool by_tile) {
+                                                 const PagedPlan& p, unsigned x) {
+  constexpr bool by_tile = WHAT != FIND_ITEM;
   const int lane = threadIdx.x & 63, each = (a.rows.B + 63) / 64;
   unsigned items = 0, tiles = 0, most = 0;
   for (int e = 0; e < each; ++e) {
@@ -189,7 +193,9 @@ __device__ __forceinline__ PagedFound paged_find(const gm_paged_attention_args& 
   PagedFound f;
   f.all_tiles = __builtin_amdgcn_readlane(st, 63);
   f.per = p.wgs ? paged_share(p, f.all_tiles, wave_max_u32(most)) : 0;
-  const unsigned at = by_tile ? x * f.per : x;
+  unsigned at = by_tile ? x * f.per : x;
+  if (WHAT == FIND_LAST && at < f.all_tiles) at = (at + f.per < f.all_tiles ? at + f.per : f.all_tiles) - 1;
+  f.at = at;
   const unsigned mine = by_tile ? tiles : items, end = by_tile ? st : si;
   const unsigned long long hit = __ballot(at < end && at >= end - mine);
   f.b = -1;
@@ -566,8 +572,15 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
       blk = plan.blocks - 1 - x;
       b = y / c.heads;
       kvh = y - b * c.heads;
+    } else if (plan.few) {
+      // (sequences of more rows are not ours, and others have one block)
+      b = blockIdx.x / c.heads;
+      kvh = blockIdx.x - b * c.heads;
+      blk = 0;
+      const int rows = paged_seq(a, c, b).n * plan.G;
+      if (rows == 0 || rows > plan.few) return;
     } else {
-      const PagedFound f = paged_find<R, UNIT>(a, c, plan, blockIdx.x, false);
+      const PagedFound f = paged_find<R, UNIT, FIND_ITEM>(a, c, plan, blockIdx.x);
       if (f.b < 0) return;
       const int x = blockIdx.x - f.items;
       b = f.b;
@@ -578,7 +591,7 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
     work(b, s, kvh, blk, s.lo & ~31, s.kend, nullptr);
     return;
   }
-  const PagedFound f = paged_find<R, UNIT>(a, c, plan, blockIdx.x, true);
+  const PagedFound f = paged_find<R, UNIT, FIND_FIRST>(a, c, plan, blockIdx.x);
   if (f.b < 0) return;
   unsigned at = blockIdx.x * static_cast<unsigned>(f.per);
   const unsigned end = at + f.per < f.all_tiles ? at + f.per : f.all_tiles;
@@ -602,88 +615,53 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
   }
 }
 
-// The parts of a cut item's row joined, a workgroup per row (token and head): the weights
-// by the first wavefront, a lane per part, then the parts in 256 / HD sets, each in order,
-// and the sets in theirs.
+// The parts of cut items joined.  A workgroup whose part of the line ends within an item that
+// began in it is the first of that item's; here (blockIdx.x) it stands for the item, whose
+// rows go to a wavefront each: the weights by a lane per part, then the parts in order.
 template <typename T, int HD, int R, int UNIT>
 __global__ __launch_bounds__(256) void k_paged_join(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
-  constexpr int SETS = 256 / HD;
-  __shared__ float s_w[64], s_o[SETS][HD];
-  const int tid = threadIdx.x, ch = tid % HD, of = tid / HD, lane = tid & 63;
-  int b, i = 0, h;
-  if (plan.joined) {
-    const int x = blockIdx.x / plan.joined, r = blockIdx.x - x * plan.joined;
-    b = x / c.heads;
-    i = r / plan.G;
-    h = (x - b * c.heads) * plan.G + r - i * plan.G;
-  } else {
-    const int token = blockIdx.x / a.n_heads;
-    h = blockIdx.x - token * a.n_heads;
-    b = a.rows.offsets ? paged_sequence_of(a.rows, token) : token / a.rows.n;
-    if (b >= a.rows.B) return;
-    i = a.rows.offsets ? token - a.rows.offsets[b] : token - b * a.rows.n;
-  }
-  // ---- tiles of the sequences before this one, and of all
-  unsigned before = 0, all = 0, most = 0;
-  for (int x = lane; x < a.rows.B; x += 64) {
-    int nb, nt;
-    paged_weight<R, UNIT>(a, c, plan, paged_seq(a, c, x), nb, nt);
-    const unsigned t = static_cast<unsigned>(nb) * c.heads * nt;
-    all += t;
-    before += x < b ? t : 0;
-    most = nb && static_cast<unsigned>(nt) > most ? nt : most;
-  }
-  all = __builtin_amdgcn_readlane(wave_scan(all), 63);
-  before = __builtin_amdgcn_readlane(wave_scan(before), 63);
-  const unsigned per = paged_share(plan, all, wave_max_u32(most));
-  const PagedSeq s = paged_seq(a, c, b);
+  constexpr int CL = (HD + 63) / 64, U = 8;    // channels of a lane, parts loaded together
+  const PagedFound f = paged_find<R, UNIT, FIND_LAST>(a, c, plan, blockIdx.x);
+  if (f.b < 0) return;
+  const PagedSeq s = paged_seq(a, c, f.b);
   int nb, nt;
   paged_weight<R, UNIT>(a, c, plan, s, nb, nt);
-  if (nb == 0 || i < 0 || i >= s.n) return;
-  const int kvh = h / plan.G, r = i * plan.G + h - kvh * plan.G, blk = r / R, row = r - blk * R;
-  const unsigned t0 = before + static_cast<unsigned>(kvh * nb + blk) * nt;
-  const unsigned w0 = t0 / per, w1 = (t0 + nt - 1) / per;
-  if (w0 == w1) return;
-  const int parts = w1 - w0 + 1;               // at most kMostParts
-  auto part = [&](int p) { return paged_part<R, HD>(a, w0 + p, p == 0, row); };
-  constexpr int U = 8;
-  float o[U];
+  const int item = (f.at - f.tiles) / nt, kvh = item / nb, blk = item - kvh * nb;
+  const unsigned t0 = f.tiles + static_cast<unsigned>(item) * nt;
+  const int parts = (t0 + nt - 1) / f.per - blockIdx.x + 1;       // at most kMostParts
+  const int row = blockIdx.y * 4 + (threadIdx.x >> 6), r = blk * R + row, lane = threadIdx.x & 63;
+  if (t0 < blockIdx.x * static_cast<unsigned>(f.per) || parts < 2 || row >= R || r >= s.n * plan.G) return;
+  auto part = [&](int p) { return paged_part<R, HD>(a, blockIdx.x + p, p == 0, row); };
+  float v[U][CL];
+  auto fetch = [&](int p0) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int p = of + u * SETS;
-    o[u] = p < parts ? part(p)[2 + ch] : 0.f;
-  }
-  if (tid < 64) {
-    const bool on = tid < parts;
-    const float m = on ? part(tid)[0] : -INFINITY, l = on ? part(tid)[1] : 0.f;
-    const float M = wave_max(m);
-    const float w = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - M);
-    const float W = wave_sum(w);
-    s_w[tid] = w == 0.f ? 0.f : w / W;
-  }
-  __syncthreads();
-  float sum = 0.f;
-  for (int p0 = 0; p0 < parts; p0 += U * SETS) {
-    if (p0) {
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int p = p0 + of + u * SETS;
-        o[u] = p < parts ? part(p)[2 + ch] : 0.f;
-      }
-    }
+      for (int e = 0; e < CL; ++e)
+        v[u][e] = p0 + u < parts && lane + 64 * e < HD ? part(p0 + u)[2 + lane + 64 * e] : 0.f;
+  };
+  fetch(0);
+  const bool on = lane < parts;
+  const float m = on ? part(lane)[0] : -INFINITY, l = on ? part(lane)[1] : 0.f;
+  const float M = wave_max(m);
+  float w = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - M);
+  const float W = wave_sum(w);
+  w = w == 0.f ? 0.f : w / W;
+  float o[CL] = {};
+  for (int p0 = 0; p0 < parts; p0 += U) {
+    if (p0) fetch(p0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int p = p0 + of + u * SETS;
-      const float w = p < parts ? s_w[p] : 0.f;
-      sum += w == 0.f ? 0.f : w * o[u];
+      const float wp = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), p0 + u));
+#pragma unroll
+      for (int e = 0; e < CL; ++e) o[e] += wp == 0.f ? 0.f : wp * v[u][e];
     }
   }
-  s_o[of][ch] = sum;
-  __syncthreads();
-  if (of) return;
+  const int i = r / plan.G;
+  T* out = paged_row_at<T>(a.out, a.rows, f.b, s.row0, i, kvh * plan.G + r - i * plan.G);
 #pragma unroll
-  for (int p = 1; p < SETS; ++p) sum += s_o[p][ch];
-  paged_row_at<T>(a.out, a.rows, b, s.row0, i, h)[ch] = from_f32<T>(sum);
+  for (int e = 0; e < CL; ++e)
+    if (lane + 64 * e < HD) out[lane + 64 * e] = from_f32<T>(o[e]);
 }
 
 // How a call is done.
@@ -712,7 +690,7 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
   // (rows of a packed call lie in at most a block a sequence more than they fill; where
   // sequences of more than a block are another kernel's, in one a sequence)
   p.items = c.heads * (!packed ? p.blocks * B : w.many ? B : static_cast<int>(most / R) + B);
-  p.joined = packed && w.many ? kFewRows : 0;
+  p.joined = static_cast<int>(std::min<int64_t>(most, R));
   const int64_t cap = static_cast<int64_t>(width) * c.page_size;
   const int64_t keys = window > 0 ? std::min<int64_t>(cap, static_cast<int64_t>(window) + n) : cap;
   const int tile = f32 ? 16 : 32;
@@ -742,7 +720,7 @@ void launch_paged_append(const gm_paged_append_args& a, hipStream_t s) {
 uint64_t paged_attention_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, int window, bool packed) {
   const PagedWay w = paged_way(c, B, n, width, n_heads, window, packed);
   // (the two kernels run one after the other)
-  const uint64_t many = w.many ? paged_prompt_workspace(c, B, n, width, n_heads, packed) : 0;
+  const uint64_t many = w.many ? paged_prompt_workspace(c, B, n, width, n_heads, w.few ? kFewRows : 0, packed) : 0;
   return w.rows_bytes > many ? w.rows_bytes : many;
 }
 
@@ -759,10 +737,9 @@ void launch_paged_attention(const gm_paged_attention_args& a, hipStream_t s) {
       constexpr int NSET = decltype(sets)::value, NWV = decltype(waves)::value, UNIT = NWV * (sizeof(T) == 4 ? 16 : 32);
       hipLaunchKernelGGL((k_paged_rows<T, HD, NSET, decltype(cap)::value, NWV>), dim3(p.wgs ? p.wgs : p.items),
                          dim3(64 * NWV), 0, s, a, c, p);
-      const int tokens = a.rows.offsets ? a.rows.n : a.rows.B * a.rows.n;
-      const int joins = p.joined ? a.rows.B * c.heads * p.joined : tokens * a.n_heads;
       if (p.wgs)
-        hipLaunchKernelGGL((k_paged_join<T, HD, 16 * NSET, UNIT>), dim3(joins), dim3(256), 0, s, a, c, p);
+        hipLaunchKernelGGL((k_paged_join<T, HD, 16 * NSET, UNIT>), dim3(p.wgs, (p.joined + 3) / 4), dim3(256), 0, s,
+                           a, c, p);
     };
     auto wide = [&](auto sets, auto cap) {
       if (w.waves == 8) go(sets, cap, std::integral_constant<int, 8>());

@@ -18,11 +18,32 @@ struct PromptPlan {
   int blocks;     // blocks of 128 rows of a key head; 0: packed, each sequence has its own
   int most;       // blocks of all sequences at the most
   int few;        // sequences of at most this many rows are another kernel's
-  int nsplit;     // parts the keys of a block are cut into at the most
+  int split;      // keys of a block may be cut into parts
 };
 
 constexpr int kRows = 128, kKeys = 64;   // a workgroup's rows, keys of a tile
+constexpr int kSlots = 512;              // workgroups that run at a time
 constexpr int kLeastTiles = 8;           // tiles a part has at the least
+
+// Parts that items (blocks and key heads) are cut into where they leave slots empty.
+__host__ __device__ inline int prompt_cuts(long long items) {
+  const long long n = items > 0 && items < kSlots / 2 ? kSlots / items : 1;
+  return n < 16 ? static_cast<int>(n) : 16;
+}
+// The cuts of a call; packed rows' blocks are counted by a wavefront.
+__device__ __forceinline__ int prompt_cuts(const gm_paged_attention_args& a, const gm_paged_cache& c, const PromptPlan& p) {
+  if (!p.split) return 1;
+  int blocks = p.most;
+  if (!p.blocks) {
+    blocks = 0;
+    for (int b = threadIdx.x & 63; b < a.rows.B; b += 64) {
+      const int rows = paged_seq(a, c, b).n * p.G;
+      blocks += rows > p.few ? (rows + kRows - 1) / kRows : 0;
+    }
+    blocks = __builtin_amdgcn_readlane(wave_scan(blocks), 63);
+  }
+  return prompt_cuts(static_cast<long long>(blocks) * c.heads);
+}
 
 // A workgroup's block of rows, and the keys it goes through.
 struct PromptPlace {
@@ -34,7 +55,7 @@ struct PromptPlace {
   int k0, k1, parts;                     // keys, from a multiple of 64; parts that the block has
 };
 __device__ __forceinline__ PromptPlace prompt_place(const gm_paged_attention_args& a, const gm_paged_cache& c,
-                                                    const PromptPlan& p, int block, int kvh, int split) {
+                                                    const PromptPlan& p, int block, int kvh, int cuts, int split) {
   PromptPlace w;
   w.kvh = kvh;
   w.split = split;
@@ -89,8 +110,8 @@ __device__ __forceinline__ PromptPlace prompt_place(const gm_paged_attention_arg
   w.k1 = w.qmax + 1 < w.s.kend ? w.qmax + 1 : w.s.kend;
   const int tiles = w.k1 > w.k0 ? (w.k1 - w.k0 + kKeys - 1) / kKeys : 0;
   w.parts = 1;
-  if (p.nsplit > 1 && tiles >= 2 * kLeastTiles) {
-    const int want = tiles / kLeastTiles < p.nsplit ? tiles / kLeastTiles : p.nsplit;
+  if (cuts > 1 && tiles >= 2 * kLeastTiles) {
+    const int want = tiles / kLeastTiles < cuts ? tiles / kLeastTiles : cuts;
     const int per = (tiles + want - 1) / want;
     w.parts = (tiles + per - 1) / per;
     w.k0 += split * per * kKeys;
@@ -101,9 +122,8 @@ __device__ __forceinline__ PromptPlace prompt_place(const gm_paged_attention_arg
 }
 
 template <int HD>
-__device__ __forceinline__ float* prompt_part(const gm_paged_attention_args& a, const PromptPlan& p, const PromptPlace& w,
-                                              int split) {
-  return static_cast<float*>(a.workspace) + (w.item * p.nsplit + split) * kRows * (HD + 2);
+__device__ __forceinline__ float* prompt_part(const gm_paged_attention_args& a, const PromptPlace& w, int cuts, int split) {
+  return static_cast<float*>(a.workspace) + (w.item * cuts + split) * kRows * (HD + 2);
 }
 
 // One, two or four instructions of 1 KB into LDS, one after the other there and, but for a
@@ -151,10 +171,12 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
 
   // heads fastest: the blocks of a key head come to one XCD where the heads are a
   // multiple of 8
+  const int cuts = prompt_cuts(a, c, plan);
   int x = blockIdx.x;
   const int kvh = x % c.heads;
   x /= c.heads;
-  const PromptPlace w = prompt_place(a, c, plan, x / plan.nsplit, kvh, x % plan.nsplit);
+  if (x >= plan.most * cuts) return;
+  const PromptPlace w = prompt_place(a, c, plan, x / cuts, kvh, cuts, x % cuts);
   if (w.b < 0 || w.split >= w.parts) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, h2 = lane >> 5;
@@ -406,7 +428,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
     for (int i = 0; i < 16; ++i) odd = fmaf(oacc[e][i], 0.f, odd);
   const unsigned long long odd_lanes = __ballot(odd != 0.f);   // (NaN != 0)
   uint32_t again = static_cast<uint32_t>(odd_lanes) | static_cast<uint32_t>(odd_lanes >> 32);
-  float* part = w.parts > 1 ? prompt_part<HD>(a, plan, w, w.split) + wave * 32 * (HD + 2) : nullptr;
+  float* part = w.parts > 1 ? prompt_part<HD>(a, w, cuts, w.split) + wave * 32 * (HD + 2) : nullptr;
   if (r < w.rows && !(again >> l32 & 1)) {
     const float inv = L > 0.f ? 1.f / L : 0.f;
     if (part) {
@@ -449,36 +471,55 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
   }
 }
 
-// The parts of a block's rows joined in order of their keys: 4 rows a workgroup, a
-// wavefront each.
+// The parts of a block's rows joined in order of their keys, a wavefront a row; 4 rows at a
+// time of at most kSlots / 2 items by a grid that fits the chip.
+constexpr int kJoins = 2048;
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_paged_prompt_join(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan) {
-  int x = blockIdx.x;
-  const int row = (x % (kRows / 4)) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  x /= kRows / 4;
-  const int kvh = x % c.heads;
-  const PromptPlace w = prompt_place(a, c, plan, x / c.heads, kvh, 0);
-  if (w.b < 0 || w.parts < 2) return;
-  const int r = w.qb * kRows + row;
-  if (r >= w.rows) return;
-  const float* part = prompt_part<HD>(a, plan, w, 0) + row * (HD + 2);
-  const int64_t step = static_cast<int64_t>(kRows) * (HD + 2);
-  const bool on = lane < w.parts;
-  const float m = on ? part[lane * step] : -INFINITY, l = on ? part[lane * step + 1] : 0.f;
-  const float M = wave_max(m);
-  float f = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - M);
-  const float F = wave_sum(f);
-  f = f == 0.f ? 0.f : f / F;
-  const int i = r / plan.G;
-  T* out = paged_row_at<T>(a.out, a.rows, w.b, w.s.row0, i, kvh * plan.G + r - i * plan.G);
+  const int cuts = prompt_cuts(a, c, plan);
+  if (cuts == 1) return;
+  constexpr int64_t STEP = kRows * (HD + 2);
+  constexpr int CL = (HD + 63) / 64, U = 4;    // channels of a lane, parts loaded together
+  const int lane = threadIdx.x & 63;
+  for (int x = blockIdx.x; x < kSlots / cuts * (kRows / 4); x += gridDim.x) {
+    const int item = x / (kRows / 4), row = x % (kRows / 4) * 4 + (threadIdx.x >> 6);
+    const int block = item / c.heads, kvh = item - block * c.heads;
+    if (block >= plan.most) return;
+    const PromptPlace w = prompt_place(a, c, plan, block, kvh, cuts, 0);
+    if (w.b < 0) return;
+    const int r = w.qb * kRows + row;
+    if (w.parts < 2 || r >= w.rows) continue;
+    const float* part = prompt_part<HD>(a, w, cuts, 0) + row * (HD + 2);
+    float v[U][CL];
+    auto fetch = [&](int p0) {
 #pragma unroll
-  for (int ch = lane; ch < HD; ch += 64) {
-    float o = 0.f;
-    for (int p = 0; p < w.parts; ++p) {
-      const float fp = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), p));
-      o += fp == 0.f ? 0.f : fp * part[p * step + 2 + ch];
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < CL; ++e)
+          v[u][e] = p0 + u < w.parts && lane + 64 * e < HD ? part[(p0 + u) * STEP + 2 + lane + 64 * e] : 0.f;
+    };
+    fetch(0);
+    const bool on = lane < w.parts;
+    const float m = on ? part[lane * STEP] : -INFINITY, l = on ? part[lane * STEP + 1] : 0.f;
+    const float M = wave_max(m);
+    float f = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - M);
+    const float F = wave_sum(f);
+    f = f == 0.f ? 0.f : f / F;
+    float o[CL] = {};
+    for (int p0 = 0; p0 < w.parts; p0 += U) {
+      if (p0) fetch(p0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float fp = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), p0 + u));
+#pragma unroll
+        for (int e = 0; e < CL; ++e) o[e] += fp == 0.f ? 0.f : fp * v[u][e];
+      }
     }
-    out[ch] = from_f32<T>(o);
+    const int i = r / plan.G;
+    T* out = paged_row_at<T>(a.out, a.rows, w.b, w.s.row0, i, kvh * plan.G + r - i * plan.G);
+#pragma unroll
+    for (int e = 0; e < CL; ++e)
+      if (lane + 64 * e < HD) out[lane + 64 * e] = from_f32<T>(o[e]);
   }
 }
 
@@ -488,27 +529,27 @@ PromptPlan prompt_plan(const gm_paged_cache& c, int B, int n, int width, int n_h
   p.few = few;
   const int64_t rows = static_cast<int64_t>(n) * p.G;      // of a key head
   p.blocks = packed ? 0 : static_cast<int>((rows + kRows - 1) / kRows);
-  p.most = packed ? static_cast<int>(rows / kRows) + B : p.blocks * B;
-  // parts that bring 512 workgroups, where the table holds so many tiles
-  const int64_t full = (packed ? (rows + kRows - 1) / kRows : p.most) * static_cast<int64_t>(c.heads);
+  // (packed: at most a block more than they fill for each sequence of more than `few` rows)
+  p.most = packed ? static_cast<int>(rows / kRows + std::min<int64_t>(B, rows / (few + 1))) : p.blocks * B;
   const int64_t tiles = static_cast<int64_t>(width) * c.page_size / kKeys;
-  int64_t want = full >= 256 ? 1 : 512 / full;
-  want = std::min<int64_t>(want, tiles / kLeastTiles);
-  p.nsplit = static_cast<int>(want < 1 ? 1 : want > 16 ? 16 : want);
+  p.split = tiles >= 2 * kLeastTiles && (packed || prompt_cuts(static_cast<int64_t>(p.most) * c.heads) > 1);
   return p;
 }
 
 }  // namespace
 
-uint64_t paged_prompt_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, bool packed) {
-  const PromptPlan p = prompt_plan(c, B, n, width, n_heads, packed, 0);
-  if (p.nsplit == 1) return 0;
-  return static_cast<uint64_t>(p.most) * c.heads * p.nsplit * kRows * (c.head_dim + 2) * sizeof(float);
+uint64_t paged_prompt_workspace(const gm_paged_cache& c, int B, int n, int width, int n_heads, int few, bool packed) {
+  const PromptPlan p = prompt_plan(c, B, n, width, n_heads, packed, few);
+  // (where blocks are cut up, their parts fill the slots at the most)
+  return p.split ? static_cast<uint64_t>(kSlots) * kRows * (c.head_dim + 2) * sizeof(float) : 0;
 }
 
 void launch_paged_prompt(const gm_paged_attention_args& a, int few, hipStream_t s) {
   const gm_paged_cache& c = *a.cache;
   const PromptPlan p = prompt_plan(c, a.rows.B, a.rows.n, a.rows.width, a.n_heads, a.rows.offsets != nullptr, few);
+  // (whole multiples of the heads)
+  const unsigned items = static_cast<unsigned>(p.most) * c.heads, slots = (kSlots + c.heads - 1) / c.heads * c.heads;
+  const unsigned grid = p.split && items < slots ? slots : items;
   const bool cap = a.scores.softcap > 0.f, bias = a.scores.slopes;
   const std::true_type yes;
   const std::false_type no;
@@ -518,15 +559,13 @@ void launch_paged_prompt(const gm_paged_attention_args& a, int few, hipStream_t 
       constexpr int HD = decltype(hd)::value;
       auto go = [&](auto cp, auto bi) {
         hipLaunchKernelGGL((k_paged_prompt<T, HD, decltype(cp)::value, decltype(bi)::value>),
-                           dim3(static_cast<unsigned>(p.most) * c.heads * p.nsplit), dim3(256), 0, s, a, c, p);
+                           dim3(grid), dim3(256), 0, s, a, c, p);
       };
       if (cap && bias) go(yes, yes);
       else if (cap) go(yes, no);
       else if (bias) go(no, yes);
       else go(no, no);
-      if (p.nsplit > 1)
-        hipLaunchKernelGGL((k_paged_prompt_join<T, HD>), dim3(static_cast<unsigned>(p.most) * c.heads * (kRows / 4)),
-                           dim3(256), 0, s, a, c, p);
+      if (p.split) hipLaunchKernelGGL((k_paged_prompt_join<T, HD>), dim3(kJoins), dim3(256), 0, s, a, c, p);
     }
   });
 }
