@@ -285,7 +285,10 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
   constexpr int NI = HD / 16;                       // products of O
   constexpr int RB = HD * ES;                       // bytes of a row
   constexpr bool F32 = ES == 4;
-  __shared__ float s_m[NWV][R], s_l[NWV][R], s_o[NWV][R][HD + 1];
+  constexpr int SO = HD + 4;                        // floats of a row of s_o
+  __shared__ __attribute__((aligned(16))) float s_o[NWV][R][SO];
+  __shared__ __attribute__((aligned(16))) float s_f[NSET == 2 ? R : 1][NWV];
+  __shared__ float s_m[NWV][R], s_l[NWV][R], s_M[NSET == 2 ? R : 1], s_L[NSET == 2 ? R : 1];
   __shared__ uint32_t s_odd;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
@@ -507,11 +510,20 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
     for (int x = 0; x < NSET; ++x) {
       l[x] += __shfl_xor(l[x], 16, 64);
       l[x] += __shfl_xor(l[x], 32, 64);
+      if (r0 + 16 * x + n > rlast) continue;
       const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int e = 0; e < 4; ++e) {
+        float v[NI];
 #pragma unroll
-        for (int y = 0; y < NI; ++y) s_o[wave][16 * x + n][NI * (4 * g + e) + y] = l[x] == 0.f ? 0.f : o[x][y][e] * inv;
+        for (int y = 0; y < NI; ++y) v[y] = l[x] == 0.f ? 0.f : o[x][y][e] * inv;
+        float* to = &s_o[wave][16 * x + n][NI * (4 * g + e)];
+        if constexpr (NI == 2) *reinterpret_cast<f32x2*>(to) = f32x2{v[0], v[1]};
+        else {
+#pragma unroll
+          for (int y = 0; y < NI; y += 4) *reinterpret_cast<f32x4*>(to + y) = f32x4{v[y], v[y + 1], v[y + 2], v[y + 3]};
+        }
+      }
       if (g == 0) {
         s_m[wave][16 * x + n] = m[x];
         s_l[wave][16 * x + n] = l[x];
@@ -519,10 +531,12 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
     }
     if (threadIdx.x == 0) s_odd = 0;
     __syncthreads();
-    for (int e = threadIdx.x; e < R * HD; e += 64 * NWV) {
-      const int ch = e % HD, row = e / HD, r = r0 + row;
-      if (r > rlast) break;
-      float M = -INFINITY, L = 0.f, O = 0.f, f[NWV];
+    // ---- the wavefronts' sums, four channels a thread.  Their weights (over the row's sum, before
+    // the products, which might pass fp32) are computed by each thread for itself where it has
+    // one or two turns, and once a row, behind a barrier more, where it has up to eight.
+    auto weights = [&](int row, float (&f)[NWV], float& M, float& L) {
+      M = -INFINITY;
+      L = 0.f;
 #pragma unroll
       for (int w = 0; w < NWV; ++w) M = fmaxf(M, s_m[w][row]);
 #pragma unroll
@@ -530,19 +544,53 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
         f[w] = s_l[w][row] == 0.f ? 0.f : s_l[w][row] * __builtin_amdgcn_exp2f(s_m[w][row] - M);
         L += f[w];
       }
-      const float inv = L == 0.f ? 0.f : 1.f / L;   // (before the products, which might pass fp32)
+      const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-      for (int w = 0; w < NWV; ++w) O += f[w] == 0.f ? 0.f : f[w] * inv * s_o[w][row][ch];
-      if (!(fabsf(O) < INFINITY) || !(L < INFINITY)) atomicOr(&s_odd, 1u << row);
+      for (int w = 0; w < NWV; ++w) f[w] *= inv;
+    };
+    if constexpr (NSET == 2) {
+      if (threadIdx.x < R && r0 + static_cast<int>(threadIdx.x) <= rlast) {
+        float f[NWV], M, L;
+        weights(threadIdx.x, f, M, L);
+#pragma unroll
+        for (int w = 0; w < NWV; ++w) s_f[threadIdx.x][w] = f[w];
+        s_M[threadIdx.x] = M;
+        s_L[threadIdx.x] = L;
+      }
+      __syncthreads();
+    }
+    for (int e = threadIdx.x; e < R * HD / 4; e += 64 * NWV) {
+      const int ch = e % (HD / 4) * 4, row = e / (HD / 4), r = r0 + row;
+      if (r > rlast) break;
+      float f[NWV], M, L;
+      if constexpr (NSET == 2) {
+#pragma unroll
+        for (int w = 0; w < NWV; ++w) f[w] = s_f[row][w];
+        M = s_M[row];
+        L = s_L[row];
+      } else {
+        weights(row, f, M, L);
+      }
+      f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NWV; ++w) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(&s_o[w][row][ch]);
+        if (f[w] != 0.f) O += f[w] * v;
+      }
+      float odd = 0.f * L;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) odd = fmaf(O[j], 0.f, odd);
+      if (odd != 0.f) atomicOr(&s_odd, 1u << row);  // (NaN != 0)
       if (part) {
-        part[row * (HD + 2) + 2 + ch] = O;
-        if (ch == 0) {
-          part[row * (HD + 2)] = M;
-          part[row * (HD + 2) + 1] = L;
-        }
+        float* to = part + row * (HD + 2) + 2 + ch;
+        *reinterpret_cast<f32x2*>(to) = f32x2{O[0], O[1]};
+        *reinterpret_cast<f32x2*>(to + 2) = f32x2{O[2], O[3]};
+        if (ch == 0) *reinterpret_cast<f32x2*>(to - 2) = f32x2{M, L};
       } else {
         const int i = r / plan.G;
-        paged_row_at<T>(a.out, a.rows, b, s.row0, i, kvh * plan.G + r - i * plan.G)[ch] = from_f32<T>(O);
+        T* to = paged_row_at<T>(a.out, a.rows, b, s.row0, i, kvh * plan.G + r - i * plan.G) + ch;
+        if constexpr (F32) *reinterpret_cast<f32x4*>(to) = O;
+        else *reinterpret_cast<u32x2*>(to) = u32x2{pack2<T>(O[0], O[1]), pack2<T>(O[2], O[3])};
       }
     }
     __syncthreads();
