@@ -203,7 +203,7 @@ __device__ __forceinline__ PagedFound paged_find(const gm_paged_attention_args& 
   const int l = __builtin_ctzll(hit);
   f.items = __builtin_amdgcn_readlane(si - items, l);
   f.tiles = __builtin_amdgcn_readlane(st - tiles, l);
-  for (int b = l * each;; ++b) {              // (ends: the lane's sequences hold it)
+  for (int b = l * each; b < a.rows.B; ++b) {  // (the lane's sequences hold it)
     int nb, nt;
     paged_weight<R, UNIT>(a, c, p, paged_seq(a, c, b), nb, nt);
     const unsigned i = static_cast<unsigned>(nb) * c.heads, t = i * nt;
@@ -214,6 +214,7 @@ __device__ __forceinline__ PagedFound paged_find(const gm_paged_attention_args& 
     f.items += i;
     f.tiles += t;
   }
+  return f;
 }
 
 // (m, l, o[HD]) of a row of a workgroup's cut item: slot 0 that begins before it, 1 after.
@@ -644,7 +645,7 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
   unsigned at = blockIdx.x * static_cast<unsigned>(f.per);
   const unsigned end = at + f.per < f.all_tiles ? at + f.per : f.all_tiles;
   unsigned first = f.tiles;                     // the sequence's first tile
-  for (int b = f.b; at < end; ++b) {
+  for (int b = f.b; at < end && b < a.rows.B; ++b) {
     const PagedSeq s = paged_seq(a, c, b);
     int nb, nt;
     paged_weight<R, UNIT>(a, c, plan, s, nb, nt);

@@ -78,6 +78,18 @@ def test_empty_and_many_packed_sequences():
     check_append(pr.Call([5] * 65, [0] * 64 + [5], 16, True), "f16", 32, 1, 1)
 
 
+def test_packed_rows_before_the_first_sequence():
+    call = pr.Call([20, 9], [5, 2], 16, True)
+    k = rand((10, 2, 64), "bf16", 1).cuda()
+    a, b = PagedCache(call.pages, 16, 2, 64), PagedCache(call.pages, 16, 2, 64)
+    (table, lengths), kw = call.device_args()
+    rotary = ops.rotary_table(call.cap, 64)
+    want = a.append(k[3:], k[3:], table, lengths, q=k[3:], rotary=rotary, **kw)
+    out = torch.full_like(k, 7.0)
+    b.append(k, k, table, lengths, offsets=kw["offsets"] + 3, q=k, q_out=out, rotary=rotary)
+    assert torch.equal(a.k, b.k) and torch.equal(a.v, b.v) and torch.equal(out[3:], want) and (out[:3] == 7).all()
+
+
 @pytest.mark.parametrize("in_place", [False, True])
 def test_rows_behind_the_last_sequence_are_left(in_place):
     check_append(pr.Call([30, 8], [5, 3], 16, True), "bf16", 64, 4, 2, extra=6, in_place=in_place)

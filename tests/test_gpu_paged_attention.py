@@ -143,6 +143,34 @@ def test_chunks_of_few_blocks_are_cut_up(dtype):
     check_attention(pr.Call([5000, 1100, 300], [40, 90, 100], 64, True), dtype, 64, 2, 1)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_packed_single_tokens_and_a_chunk_among_them(dtype):
+    new = [1] * 200
+    check_attention(pr.Call([(b * 37) % 300 + 1 for b in range(200)], new, 16, True), dtype, 64, 4, 2)
+    new[77] = 150
+    check_attention(pr.Call([(b * 37) % 300 + n for b, n in enumerate(new)], new, 16, True), dtype, 64, 4, 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 50])
+def test_packed_rows_before_the_first_sequence(dtype, n):
+    """offsets may begin behind row 0: rows before it are no sequence's."""
+    call = pr.Call([150, 99], [n, n], 16, False)
+    cache, q = pools(call, dtype, 2, 64), rand((4 + 2 * n, 4, 64), dtype, 9).cuda()
+    (table, lengths), _ = call.device_args()
+    out = torch.full_like(q, 7.0)
+    paged_attention(q, cache, table, lengths, offsets=torch.tensor([4, 4 + n, 4 + 2 * n], dtype=torch.int32, device="cuda"), out=out)
+    want = paged_attention(q[4:], cache, table, lengths, offsets=torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda"))
+    assert (out[:4] == 7.0).all() and torch.equal(out[4:], want)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("n", [1, 60])
+def test_a_scale_of_its_own(dtype, n):
+    check_attention(pr.Call([200, 77], [n, n], 16, False), dtype, 64, 4, 2, scale=0.5)
+    check_attention(pr.Call([200, 77], [n, n], 16, False), dtype, 64, 4, 2, scale=1e-3, softcap=2.0)
+
+
 # ------------------------------------------------------------ windows and holes
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 64, 100, 1000])
@@ -320,6 +348,25 @@ def test_offsets_past_32_bits():
         a = paged_attention(q, cache, at.int()[None], lengths)
         b = paged_attention(q, few, torch.tensor([[0, 1, 2]], dtype=torch.int32, device="cuda"), lengths)
         assert torch.equal(a, b)
+
+
+def test_wrong_calls_raise():
+    cache = PagedCache(4, 16, 2, 64)
+    t, n = torch.zeros((1, 3), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 1, 3, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(gm.GmError, match="multiple of the cache's heads"):
+        paged_attention(q, cache, t, n)
+    k = q[:, :, :2].contiguous()
+    with pytest.raises(gm.GmError, match="every position"):
+        cache.append(k, k, t, n, rotary=ops.rotary_table(40, 64))
+    with pytest.raises(gm.GmError, match="window"):
+        paged_attention(k, cache, t, n, window=-3)
+    with pytest.raises(gm.GmError, match="overlap"):
+        paged_attention(k, cache, t, n, out=k)
+    with pytest.raises(ValueError, match="table must"):
+        paged_attention(k, cache, t.cpu(), n)
+    with pytest.raises(ValueError, match="q must be"):
+        paged_attention(k.cpu(), cache, t, n)
 
 
 def test_nothing_to_do():

@@ -209,3 +209,19 @@ def test_wrappers_refuse_bad_calls():
     # codes of the C entry come back as numbers: a window below 0 and one past an int
     assert attend(window=-1) == gm.GM_E_INVAL and attend(window=1 << 40) == gm.GM_E_INVAL
     assert append(cos=r[:40], sin=r[:40]) == gm.GM_E_INVAL and b"every position" in gm.lib().gm_last_error()
+
+
+def test_rotary_tables():
+    """Against the angles by Python's own arithmetic, rounded once: half a step of float32 of the
+    value, and what an angle of up to 5000 loses in float64, 5000 * 2^-52."""
+    import math
+    cos, sin = ops.rotary_table(5000, 64, base=500.0, device="cpu")
+    assert cos.shape == sin.shape == (5000, 32) and cos.dtype == sin.dtype == torch.float32
+    assert (cos[0] == 1).all() and (sin[0] == 0).all()
+    for p in (1, 77, 4999):
+        for c in (0, 1, 17, 31):
+            angle = p * 500.0 ** (-2 * c / 64)
+            for got, want in ((cos, math.cos(angle)), (sin, math.sin(angle))):
+                assert abs(float(got[p, c]) - want) <= 2.0 ** -24 * abs(want) + 4 * 5000 * 2.0 ** -52
+    assert ops.rotary_table(0, 64, device="cpu")[0].shape == (0, 32)
+    assert ops.rotary_table(8, 0, device="cpu")[1].shape == (8, 0)
