@@ -16,10 +16,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------ append
 //
-// A workgroup takes one token: its query, key and value heads in one line, a thread 16
-// channels of a head, the two halves of 8 pairs (lo, hi) that turn together (of
-// channels that do not turn: 16 in a row).  256 is a multiple of a head's threads, so a
-// thread's channels and its cosines and sines are the same for all of its heads.
+// TPT threads, a wavefront or the workgroup, take one token: its query, key and value heads in
+// one line, a thread 16 channels of a head, the two halves of 8 pairs (lo, hi) that turn
+// together (of channels that do not turn: 16 in a row).  TPT is a multiple of a head's
+// threads, so a thread's channels and its cosines and sines are the same for all of its heads.
 template <typename T> struct Half8 {       // 8 channels
   static constexpr int NV = static_cast<int>(sizeof(T)) / 2;
   u32x4 raw[NV];
@@ -35,11 +35,13 @@ template <typename T> struct Half8 {       // 8 channels
   __device__ __forceinline__ void set(int i, float x) { reinterpret_cast<T*>(raw)[i] = from_f32<T>(x); }
 };
 
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm_paged_cache c) {
-  constexpr int LPR = HD / 16, U = 4, STEP = 256 / LPR;
+template <typename T, int HD, int TPT>
+__global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm_paged_cache c, int tokens) {
+  constexpr int LPR = HD / 16, U = 4, STEP = TPT / LPR;
   const gm_paged_rows& r = a.rows;
-  const int row = blockIdx.x, nq = a.n_q_heads, heads = nq + 2 * c.heads;
+  const int nq = a.n_q_heads, heads = nq + 2 * c.heads;
+  const int row = TPT == 256 ? blockIdx.x : blockIdx.x * (256 / TPT) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPT);
+  if (row >= tokens) return;
   const int ch = threadIdx.x % LPR;
   const bool turns = ch < a.rot / 16;
   // packed rows are one sequence as far as their tensors go
@@ -60,7 +62,7 @@ __global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm
       hi[u].load(x + to(h));
     }
   };
-  const int h1 = threadIdx.x / LPR;
+  const int h1 = threadIdx.x % TPT / LPR;
   fetch(h1);                                 // (on their way while the place is looked up)
   // ---- whose token this is, and its position
   const int b = r.offsets ? paged_sequence_of(r, row) : first;
@@ -729,7 +731,10 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
   const int G = n_heads / c.heads;
   const int64_t most = static_cast<int64_t>(n) * G;        // rows of a key head of one sequence
   w.many = !f32 && most > kFewRows;
-  w.few = !w.many || packed;
+  const int64_t cap = static_cast<int64_t>(width) * c.page_size;
+  // (of a packed call, some sequences may be of few rows; over short caches the prompt kernel
+  // takes them too)
+  w.few = !w.many || (packed && cap > 512);
   w.nset = most > 16 ? 2 : 1;
   const int R = 16 * w.nset;
   PagedPlan& p = w.rows;
@@ -740,14 +745,14 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
   // sequences of more than a block are another kernel's, in one a sequence)
   p.items = c.heads * (!packed ? p.blocks * B : w.many ? B : static_cast<int>(most / R) + B);
   p.joined = static_cast<int>(std::min<int64_t>(most, R));
-  const int64_t cap = static_cast<int64_t>(width) * c.page_size;
   const int64_t keys = window > 0 ? std::min<int64_t>(cap, static_cast<int64_t>(window) + n) : cap;
   const int tile = f32 ? 16 : 32;
   const double item_us = keys * c.head_dim * (f32 ? 8. : 4.) / 46e3, all_us = item_us * p.items * (46e3 / 4.9e6);
   p.wgs = 0;
   w.waves = 8;
   if (p.items > 512 || keys <= 8 * tile) w.waves = 4;
-  if (p.items < 1024 && (item_us > 25. || item_us > all_us + 5.)) {
+  // (sequences of few rows beside chunks of many: a launch less for up to 7 us more)
+  if (p.items < 1024 && (item_us > 25. || item_us > all_us + (w.many ? 12. : 5.))) {
     const int64_t tiles = (keys + tile * 4 - 1) / (tile * 4) * p.items;
     w.waves = tiles >= 512 ? 8 : 4;
     p.wgs = static_cast<int>(tiles >= 512 ? 256 : tiles);
@@ -760,9 +765,17 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
 
 void launch_paged_append(const gm_paged_append_args& a, hipStream_t s) {
   const gm_paged_cache& c = *a.cache;
-  const unsigned tokens = static_cast<unsigned>(a.rows.offsets ? a.rows.n : a.rows.B * a.rows.n);
+  const int tokens = a.rows.offsets ? a.rows.n : a.rows.B * a.rows.n;
+  // a wavefront a token where its heads fill one no more than twice, and tokens are many
+  // (TOKENFIG)
+  const bool small = (a.n_q_heads + 2 * c.heads) * (c.head_dim / 16) <= 128 && tokens >= 512;
   by_paged_cache(c, [&](auto t, auto hd) {
-    hipLaunchKernelGGL((k_paged_append<decltype(t), decltype(hd)::value>), dim3(tokens), dim3(256), 0, s, a, c);
+    typedef decltype(t) T;
+    constexpr int HD = decltype(hd)::value;
+    if (small)
+      hipLaunchKernelGGL((k_paged_append<T, HD, 64>), dim3((tokens + 3) / 4), dim3(256), 0, s, a, c, tokens);
+    else
+      hipLaunchKernelGGL((k_paged_append<T, HD, 256>), dim3(tokens), dim3(256), 0, s, a, c, tokens);
   });
 }
 

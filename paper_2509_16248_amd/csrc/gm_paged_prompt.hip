@@ -532,7 +532,9 @@ PromptPlan prompt_plan(const gm_paged_cache& c, int B, int n, int width, int n_h
   // (packed: at most a block more than they fill for each sequence of more than `few` rows)
   p.most = packed ? static_cast<int>(rows / kRows + std::min<int64_t>(B, rows / (few + 1))) : p.blocks * B;
   const int64_t tiles = static_cast<int64_t>(width) * c.page_size / kKeys;
-  p.split = tiles >= 2 * kLeastTiles && (packed || prompt_cuts(static_cast<int64_t>(p.most) * c.heads) > 1);
+  // (of packed rows, those that must lie in blocks)
+  const int64_t least = packed ? std::max<int64_t>(0, rows - static_cast<int64_t>(B) * few + kRows - 1) / kRows : p.most;
+  p.split = tiles >= 2 * kLeastTiles && prompt_cuts(std::max<int64_t>(least, 1) * c.heads) > 1;
   return p;
 }
 
