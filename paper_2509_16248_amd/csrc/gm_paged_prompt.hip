@@ -23,7 +23,10 @@ struct PromptPlan {
 
 constexpr int kRows = 128, kKeys = 64;   // a workgroup's rows, keys of a tile
 constexpr int kSlots = 512;              // workgroups that run at a time
-constexpr int kLeastTiles = 8;           // tiles a part has at the least
+// Tiles a part has at the least, and a table whose calls cut blocks at all, which takes the
+// join's launch (parts of 8 / 3 tiles: 4 packed chunks of 713 tokens of 1024, one head of 64, 24.6 /
+// 18.8 us; but 600 tokens, 12 heads of 64, whole 12.2, cut 15.5).
+constexpr int kLeastTiles = 3, kSplitTiles = 16;
 
 // Parts that items (blocks and key heads) are cut into where they leave slots empty.
 __host__ __device__ inline int prompt_cuts(long long items) {
@@ -534,7 +537,7 @@ PromptPlan prompt_plan(const gm_paged_cache& c, int B, int n, int width, int n_h
   const int64_t tiles = static_cast<int64_t>(width) * c.page_size / kKeys;
   // (of packed rows, those that must lie in blocks)
   const int64_t least = packed ? std::max<int64_t>(0, rows - static_cast<int64_t>(B) * few + kRows - 1) / kRows : p.most;
-  p.split = tiles >= 2 * kLeastTiles && prompt_cuts(std::max<int64_t>(least, 1) * c.heads) > 1;
+  p.split = tiles >= kSplitTiles && prompt_cuts(std::max<int64_t>(least, 1) * c.heads) > 1;
   return p;
 }
 
