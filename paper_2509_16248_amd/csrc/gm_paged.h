@@ -18,8 +18,8 @@ __device__ __forceinline__ int32_t const_load(const int32_t* p) {
   return *(cptr)reinterpret_cast<uintptr_t>(p);
 }
 
-// 16 bytes of LDS, as lds_read_tr16 reads them: the compiler makes such a read wait for
-// every copy into LDS in flight, and each before the next.  lgkm_wait16() must precede any use.
+// 16 bytes of LDS, as lds_read_tr16 reads them: the compiler makes such a read wait for every
+// copy into LDS in flight, and for the read before it.  lgkm_wait16() must precede any use.
 template <int OFF>
 __device__ __forceinline__ u32x4 lds_read16(uint32_t addr) {
   u32x4 v;

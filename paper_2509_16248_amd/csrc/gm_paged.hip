@@ -16,6 +16,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------ append
 //
+// Moves bytes: a token's query, key and value rows once each way, and its row of cosines and
+// sines.  What a small call waits for is the chain offsets - length - table entry - store, so
+// the rows are fetched before their place is looked up (8 tokens of 12 heads of 64: 3.8 ->
+// 3.4 us; eight packed chunks, 16,000 tokens of 32/8 heads of 128, fp16, 86 -> 78 us, 5.2 TB/s;
+// 2048 tokens of 32 heads 17.8 us, 5.7 TB/s, partly from the Infinity Cache).
 // TPT threads, a wavefront or the workgroup, take one token: its query, key and value heads in
 // one line, a thread 16 channels of a head, the two halves of 8 pairs (lo, hi) that turn
 // together (of channels that do not turn: 16 in a row).  TPT is a multiple of a head's
@@ -130,8 +135,9 @@ __global__ __launch_bounds__(256) void k_paged_append(gm_paged_append_args a, gm
 
 // ------------------------------------------------------------ attention of a few tokens
 //
-// The rows of a key head (its query heads times the new tokens) come in blocks of R = 16 or
-// 32; an item is such a block.  Its keys go through in tiles; where items are few they are
+// Reads every seen key and value once per block of rows: memory bounds it, at 5.3 to 5.5 TB/s
+// of the long caches (a large copy moves 4.89).  The rows of a key head (its query heads times
+// the new tokens) come in blocks of R = 16 or 32; an item is such a block.  Its keys go through in tiles; where items are few they are
 // cut up: all tiles of all items in one line, and each of `wgs` workgroups takes an equal
 // part of it, whatever the lengths are (one of 32 sequences long, the others short).  A
 // workgroup then has the end of one item, whole ones, and the start of another; the two
@@ -275,6 +281,10 @@ constexpr int rows_waves(int hd, int nset) { return hd == 128 || nset == 2 ? 2 :
 // slots of its operand of P: P needs no exchange.  V comes in rows, HD / 16 channels of a
 // key a lane, row m of product e being channel (HD / 16) m + e; in 16 bits a byte permute per
 // word puts two keys of a channel together.
+// 16-bit weights are rounded to the type for the second product (half a step of each, 2^-9 or
+// 2^-12 of it; their sum takes them unrounded): its operands are 16-bit.
+// The two tiles of NSET = 1 take 64 registers each at 128 channels; with 32 rows there is one,
+// whose K and V are fetched again as soon as each has been used.
 // The maximum m moves lazily (by more than 2^8).  Hidden keys have weight 0, and values that
 // no row sees are cleared (a page's unused end may hold anything); rows that still come out
 // not finite are computed again by paged_row, which skips what is hidden.
@@ -723,7 +733,22 @@ struct PagedWay {
   uint64_t rows_bytes; // workspace of the former
 };
 
-constexpr int kFewRows = 32;       // query rows of a key head up to which the rows kernel takes 16 bits
+// Query rows of a key head up to which the rows kernel takes 16 bits (prompt kernel / rows
+// kernel, bf16: 4 sequences of 600 and 6000 keys, 32/8 heads of 128, 36 rows 17.5 / 18.7 and
+// 33.0 / 47.5; 8 of 140 and 2000, 12 heads of 64, 33 rows 7.8 / 10.7 and 26.5 / 22.2; 16 of 2000,
+// 32/8 heads of 128, 64 rows 44.3 / 39.7, 132 rows 51.2 / 80.0).
+constexpr int kFewRows = 32;
+
+// Whole items, or all tiles shared out.  A CU draws 46 GB/s at the most (one item of 4000 keys,
+// 8 key heads of 128, whole 44.4 us), the chip 5 TB/s; sharing costs the join's launch and the
+// ends of cut items, 5 us and more (us whole / shared by 256 workgroups of 8 wavefronts / by 512
+// of 4: 8 sequences of 640 keys, 12 heads of 64, 9.0 / 13.1 / 13.0; 24 of 1028, 32/8 heads of
+// 128, five tokens, 24.3 / 39.6 / 43.3; 32 of 1000 25.1 / 32.0 / 33.1, of 8190 159 / 162 / 164;
+// one of 1000 15.4 / 13.6 / 12.4, of 32000 with 32 key heads 350 / 98.5 / 100; four of 1500 20.6
+// / 14.8 / 15.7; one of 8190 among 31 of 300 102 / 27.8 / 29.5).  Only the table's capacity is
+// known on the host, so an item that could take 25 us is never whole: the lengths may be
+// anything.  8 wavefronts a whole item: 16 sequences of 1000 keys, 8 heads of 32, 8.4 us, with 4
+// 9.7; 2048 items of 700 keys 103.8 and 102.6.
 
 PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads, int window, bool packed) {
   PagedWay w;
@@ -733,7 +758,8 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
   w.many = !f32 && most > kFewRows;
   const int64_t cap = static_cast<int64_t>(width) * c.page_size;
   // (of a packed call, some sequences may be of few rows; over short caches the prompt kernel
-  // takes them too)
+  // takes them too, for a launch less: 4 chunks of 100 tokens, 12 heads of 64, of 500 keys 11.2
+  // us, with both kernels 12.9)
   w.few = !w.many || (packed && cap > 512);
   w.nset = most > 16 ? 2 : 1;
   const int R = 16 * w.nset;
@@ -766,9 +792,11 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
 void launch_paged_append(const gm_paged_append_args& a, hipStream_t s) {
   const gm_paged_cache& c = *a.cache;
   const int tokens = a.rows.offsets ? a.rows.n : a.rows.B * a.rows.n;
-  // a wavefront a token where its heads fill one no more than twice, and tokens are many
-  // (TOKENFIG)
-  const bool small = (a.n_q_heads + 2 * c.heads) * (c.head_dim / 16) <= 128 && tokens >= 512;
+  // A wavefront a token where tokens are many and a head's threads times heads fill it six
+  // times at the most (us with a wavefront / a workgroup a token, bf16: 4000 tokens of 2/2
+  // heads of 64 4.6 / 6.7, of 12/12 8.4 / 9.8, of 32/8 heads of 128 17.7 / 18.1; but 2048 of 32/32
+  // 19.5 / 18.0, and 400 of 12/12 heads of 64 4.7 / 3.9).
+  const bool small = (a.n_q_heads + 2 * c.heads) * (c.head_dim / 16) <= 384 && tokens >= 1024;
   by_paged_cache(c, [&](auto t, auto hd) {
     typedef decltype(t) T;
     constexpr int HD = decltype(hd)::value;

@@ -151,13 +151,26 @@ constexpr int paged_prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 :
 // (gm_attention_prompt.hip) splits and multiplies: 4 wavefronts x 32 rows, key and value
 // tiles of 64 keys double-buffered in LDS, S^T = K Q^T and O^T += V^T P^T on 32x32x16, a
 // lane holding 32 scores of one row per tile, the running maximum moved lazily.
-// A copy instruction fills 4, 8 or 16 rows, which lie in one page (pages are multiples of
-// 16): the page comes from a word per lane, the tile's 64 table entries, read a tile
-// ahead, and the entries that are no page give the tile's holes in a ballot.  Rows past
-// the last key repeat it.
+// A wavefront copies 16 rows of a tile, which lie in one page (pages are multiples of 16): a
+// word per lane holds the tile's 64 table entries, read a tile ahead, one of which gives the
+// scalar address, and those that are no page give the tile's holes in a ballot.  Rows past
+// the last key repeat it.  (Addresses by lane: 300 vector instructions a tile, 60.6 us for the
+// 2048 tokens below; so 52.9.)
+// LDS is read ahead of the products by hand: K two k steps, V one of 16 keys (left to the
+// compiler each K operand's read waits for the one before: 2 us more).
+// Probabilities are rounded to T for the second product (half a step of each, 2^-9 or 2^-12
+// of it; their sum takes them unrounded): its operands are 16-bit.
 // A hidden key has probability 0, but 0 times an Inf or NaN value is NaN in the matrix
 // product: rows whose sums came out not finite are computed again by paged_row, which skips
 // hidden keys.
+// Measured, bf16, 32 heads of 128, launches one after the other: 2048 tokens 48 to 51 us (700
+// TFLOP/s; capped 57, biased 56), 4 x 2048 with 8 key heads 154 (890), 8192 tokens 530 (1040; a
+// large matrix product reaches 1197), 512 tokens behind 7680 85 (770).  What bounds it: a SIMD's
+// two wavefronts keep the matrix cores busy 46% and the vector units 42% of the time that CUs
+// hold work, each wavefront's own chain of instructions taking the rest.  Not faster: the next
+// tile's scores beside this one's probabilities in one wavefront (the registers of two score
+// tiles spill, 2 x slower; at one wavefront per SIMD without spilling 1.6 x), halves of a tile
+// in turn (54.7 us against 52.9), more than one running sum or maximum, wavefront priorities.
 template <typename T, int HD, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(paged_prompt_waves(HD), paged_prompt_waves(HD))))
 void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan) {
