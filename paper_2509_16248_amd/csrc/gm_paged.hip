@@ -792,11 +792,11 @@ PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads
 void launch_paged_append(const gm_paged_append_args& a, hipStream_t s) {
   const gm_paged_cache& c = *a.cache;
   const int tokens = a.rows.offsets ? a.rows.n : a.rows.B * a.rows.n;
-  // A wavefront a token where tokens are many and a head's threads times heads fill it six
-  // times at the most (us with a wavefront / a workgroup a token, bf16: 4000 tokens of 2/2
-  // heads of 64 4.6 / 6.7, of 12/12 8.4 / 9.8, of 32/8 heads of 128 17.7 / 18.1; but 2048 of 32/32
-  // 19.5 / 18.0, and 400 of 12/12 heads of 64 4.7 / 3.9).
-  const bool small = (a.n_q_heads + 2 * c.heads) * (c.head_dim / 16) <= 384 && tokens >= 1024;
+  // A wavefront a token where tokens are many and a head's threads times heads fill it three
+  // times at the most (us with a wavefront / a workgroup a token: bf16, 4000 tokens of 2/2
+  // heads of 64 4.6 / 6.7, of 12/12 8.4 / 9.8, of 32/8 heads of 128 17.7 / 18.1; but 16,000 of
+  // those in fp16 82.0 / 78.4, 2048 of 32/32 19.5 / 18.0, and 400 of 12/12 heads of 64 4.7 / 3.9).
+  const bool small = (a.n_q_heads + 2 * c.heads) * (c.head_dim / 16) <= 192 && tokens >= 1024;
   by_paged_cache(c, [&](auto t, auto hd) {
     typedef decltype(t) T;
     constexpr int HD = decltype(hd)::value;
