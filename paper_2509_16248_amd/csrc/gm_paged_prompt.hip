@@ -141,8 +141,8 @@ __device__ __forceinline__ void copy_rows(const char* g, const uint32_t (&off)[2
 __device__ __forceinline__ void copy_rows(const char* g, const uint32_t (&off)[4], void* lds) {
   __builtin_amdgcn_global_load_lds(g + off[0], (lds_vptr)lds, 16, 0, 0);
   __builtin_amdgcn_global_load_lds(g + off[1], (lds_vptr)lds, 16, 1024, 0);
-  __builtin_amdgcn_global_load_lds(g + off[2], (lds_vptr)lds, 16, 2048, 0);
-  __builtin_amdgcn_global_load_lds(g + off[3], (lds_vptr)lds, 16, 3072, 0);
+  __builtin_amdgcn_global_load_lds(g + off[2], (lds_vptr)lds, 16, 2 * 1024, 0);
+  __builtin_amdgcn_global_load_lds(g + off[3], (lds_vptr)lds, 16, 3 * 1024, 0);
 }
 
 constexpr int paged_prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 : 4; }

@@ -185,7 +185,12 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     } else if (a[10] != Py_None) {
       refuse("q_out needs q");
     }
-    const int rc = gm_paged_append(&g, stream_at(a[11]));
+    const hipStream_t stream = stream_at(a[11]);
+    int rc;
+    // (a launch may wait for room in the queue)
+    Py_BEGIN_ALLOW_THREADS
+    rc = gm_paged_append(&g, stream);
+    Py_END_ALLOW_THREADS
     if (rc) return PyLong_FromLong(rc);
     if (a[9] == Py_None) Py_RETURN_NONE;
     return returned(a[10], out);
@@ -219,7 +224,11 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       work = at::empty({static_cast<int64_t>(g.workspace_bytes)}, q.options().dtype(at::kByte));
       g.workspace = work.data_ptr();
     }
-    const int rc = gm_paged_attention(&g, stream_at(a[11]));
+    const hipStream_t stream = stream_at(a[11]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = gm_paged_attention(&g, stream);
+    Py_END_ALLOW_THREADS
     return rc ? PyLong_FromLong(rc) : returned(a[10], out);
   });
 }
