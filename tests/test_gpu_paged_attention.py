@@ -453,3 +453,35 @@ def test_graphs_of_two_calls_replayed_in_turn():
             eager = paged_attention(qs[i], caches[i], *args[i])
             assert torch.equal(outs[i], want[i]) and torch.equal(eager, want[i])
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("packed", [False, True])
+def test_a_captured_call_follows_lengths_offsets_and_tables(dtype, packed):
+    """What the arrays hold at each replay counts: sequences that grow, move to other pages, take
+    other shares of the packed rows, or have none."""
+    B, width, ps, H, Hkv, hd, total = 4, 250, 16, 4, 2, 64, 130
+    cache = PagedCache.of(*(rand((B * width, Hkv, ps, hd), dtype, s).cuda() for s in (2, 3)))
+    q = rand((total, H, hd) if packed else (B, 2, H, hd), dtype, 4).cuda()
+    table = torch.zeros((B, width), dtype=torch.int32, device="cuda")
+    lengths, offsets = torch.ones(B, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    out = torch.zeros_like(q)
+    kw = {"offsets": offsets} if packed else {}
+    paged_attention(q, cache, table, lengths, out=out, **kw)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        paged_attention(q, cache, table, lengths, out=out, **kw)
+    for i, (length, new) in enumerate([([4000, 3, 900, 60], [100, 1, 0, 29]), ([130, 4000, 4000, 2000], [1, 1, 1, 1]),
+                                       ([0, 0, 0, 0], [0, 0, 0, 0]), ([150, 2, 3999, 700], [130, 0, 0, 0]),
+                                       ([40, 41, 42, 43], [33, 32, 31, 34])]):
+        table.copy_(torch.randperm(B * width, generator=torch.Generator().manual_seed(i)).reshape(B, width).int())
+        lengths.copy_(torch.tensor(length, dtype=torch.int32))
+        offsets.copy_(torch.tensor([sum(new[:b]) for b in range(B + 1)], dtype=torch.int32))
+        out.fill_(7.0)
+        want = torch.full_like(q, 7.0)
+        g.replay()
+        paged_attention(q, cache, table, lengths, out=want, **kw)
+        assert torch.equal(out, want), i
+        if packed:
+            assert (out[sum(new):] == 7.0).all()
+        torch.cuda.synchronize()
