@@ -11,6 +11,13 @@ namespace gm {
 
 constexpr float kPagedLog2e = 1.4426950408889634f;
 
+// fp16 weights go into the matrix products times 2^7 (the largest is 2^15): fewer fall below the
+// type's smallest normal.  Their sum is then that much too large, which a row's output, divided by
+// it, does not show; a part in the workspace holds the sum without the factor (times kWeightDown),
+// as paged_row returns it, so that parts computed either way may be joined.
+template <typename T> constexpr float kWeightUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
+template <typename T> constexpr float kWeightDown = std::is_same<T, f16_t>::value ? 0x1p-7f : 1.f;
+
 // Memory that no kernel writes while it is read here, by a scalar load where the
 // address is the same for every lane.
 __device__ __forceinline__ int32_t const_load(const int32_t* p) {
@@ -99,7 +106,7 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
 // weights' sum, then the output, of weights that add up to 1, so that it overflows only
 // where it has to.  A hidden key is skipped, so that nothing its value holds can reach
 // the sums.  store(channel, value) for every channel; the row's largest score (log2
-// units) and sum are returned.
+// units) and its sum of exp2(score - largest) are returned.
 template <typename T, int HD, typename F>
 __device__ __forceinline__ f32x2 paged_row(const gm_paged_attention_args& a, const gm_paged_cache& c,
                                            const PagedSeq& s, int b, int h, int i, int k0, int k1, F store) {

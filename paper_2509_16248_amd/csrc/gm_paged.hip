@@ -440,9 +440,7 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
 #pragma unroll
           for (int e = 0; e < NI; ++e) o[x][e] *= f;
         }
-        // fp16 weights times 2^7 (at most 2^15): fewer fall below its smallest normal
-        constexpr float kUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
-        const float msub = m[x] == -INFINITY ? 0.f : m[x] - kUp;
+        const float msub = m[x] == -INFINITY ? 0.f : m[x] - kWeightUp<T>;
 #pragma unroll
         for (int j = 0; j < NS; ++j) {
           sc[x][j] = __builtin_amdgcn_exp2f(sc[x][j] - msub);
@@ -598,7 +596,7 @@ void k_paged_rows(gm_paged_attention_args a, gm_paged_cache c, PagedPlan plan) {
         float* to = part + row * (HD + 2) + 2 + ch;
         *reinterpret_cast<f32x2*>(to) = f32x2{O[0], O[1]};
         *reinterpret_cast<f32x2*>(to + 2) = f32x2{O[2], O[3]};
-        if (ch == 0) *reinterpret_cast<f32x2*>(to - 2) = f32x2{M, L};
+        if (ch == 0) *reinterpret_cast<f32x2*>(to - 2) = f32x2{M, L * kWeightDown<T>};
       } else {
         const int i = r / plan.G;
         T* to = paged_row_at<T>(a.out, a.rows, b, s.row0, i, kvh * plan.G + r - i * plan.G) + ch;

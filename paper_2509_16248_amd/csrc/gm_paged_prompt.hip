@@ -357,8 +357,6 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
         for (int i = 0; i < 16; ++i)
           sacc[kk][i] = (vis >> (32 * kk + 8 * (i >> 2) + (i & 3))) & 1ull ? sacc[kk][i] : -INFINITY;
     }
-    // fp16 probabilities times 2^7 (at most 2^15): fewer fall below its smallest normal
-    constexpr float kUp = std::is_same<T, f16_t>::value ? 7.f : 0.f;
     float mx = -INFINITY;
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk)
@@ -374,7 +372,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
       for (int e = 0; e < CB; ++e) oacc[e] *= alpha;
       mrun = mnew;
     }
-    const float msub = mrun == -INFINITY ? 0.f : mrun - kUp;
+    const float msub = mrun == -INFINITY ? 0.f : mrun - kWeightUp<T>;
     // ---- O^T += V^T P^T: four 16-key steps; the V^T operands of step k2 + 1 are read
     // while step k2 multiplies, those of the first while the probabilities are computed
     vec pb[4];
@@ -449,7 +447,7 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
     const float inv = L > 0.f ? 1.f / L : 0.f;
     if (part) {
       float* o = part + l32 * (HD + 2);
-      if (h2 == 0) *reinterpret_cast<f32x2*>(o) = f32x2{mrun, L};
+      if (h2 == 0) *reinterpret_cast<f32x2*>(o) = f32x2{mrun, L * kWeightDown<T>};
 #pragma unroll
       for (int e = 0; e < CB; ++e)
 #pragma unroll

@@ -237,6 +237,30 @@ def test_inf_and_nan_reach_only_who_sees_them(dtype, n):
     assert torch.isnan(got[0, 0, 2:, 7]).all() and torch.isfinite(got[0, 1:].float()).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 4, 60])
+@pytest.mark.parametrize("where", ["last token", "before the window", "seen by all", "hole"])
+def test_inf_and_nan_in_a_part_of_a_cut_row(dtype, n, where):
+    """Long rows are cut along the keys; one of the parts holds the value that is not finite."""
+    length, window = 5200, 4001 if where == "before the window" else 0
+    call = pr.Call([length], [n], 16, False)
+    call.table, call.pages = call.table + 1, call.pages + 1    # page 0 is nobody's: all of it NaN
+    if where == "hole":
+        call.table[0, 150:153] = torch.tensor([-1, 10 ** 6, -1], dtype=torch.int32)
+        call.table[0, 290] = -1
+
+    def change(call, q, kp, vp):
+        p = {"last token": length - 1, "before the window": length - n - window, "seen by all": 2000}.get(where)
+        if p is not None:
+            at = call.place(0, p)
+            vp[at[0], 0, at[1], 5] = float("inf")
+
+    got = check_attention(call, dtype, 64, 4, 2, change=change, window=window).cpu()[0].float()
+    rows = {"last token": slice(n - 1, n), "seen by all": slice(0, n)}.get(where, slice(0, 0))
+    assert torch.isinf(got[rows, :2, 5]).all()
+    assert int((~torch.isfinite(got)).sum()) == 2 * got[rows].shape[0]
+
+
 @pytest.mark.parametrize("dtype,top", [("bf16", 3.3e38), ("f16", 65504.0), ("f32", 3.3e38)])
 @pytest.mark.parametrize("n,length", [(1, 90), (40, 90), (1, 2600), (40, 2600)])
 def test_averages_of_the_largest_values_are_finite(dtype, top, n, length):
