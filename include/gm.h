@@ -556,7 +556,8 @@ typedef struct gm_paged_cache {
  *           stored there and nobody sees its positions.  Entries past a
  *           sequence's length are not followed.
  * width * page_size positions, at most 2^24, are what a sequence can hold; a
- * token at a negative position, as where lengths[b] < n_b, belongs nowhere.
+ * token at a negative position, as where lengths[b] < n_b, belongs nowhere, nor
+ * does one past them.  A length may be any int32; one below 0 counts as 0.
  * All arrays are read on the device. */
 typedef struct gm_paged_rows {
   int32_t B, n, width;

@@ -57,7 +57,12 @@ __device__ __forceinline__ PagedSeq paged_seq(const gm_paged_attention_args& a, 
   }
   const int len = const_load(a.rows.lengths + b), cap = a.rows.width * c.page_size;
   s.kend = len < 0 ? 0 : len < cap ? len : cap;
+  // lengths may hold anything: a token that lies past the table by the window sees nothing, and
+  // without a window everything, with the same weights wherever it is (a bias falls by as much for
+  // every key), so positions end there and the sums made of them stay below 2^26
+  const int last = cap + a.window;
   s.p0 = (len < 0 ? 0 : len) - s.n;
+  s.p0 = s.p0 < last ? s.p0 : last;
   s.lo = a.window > 0 && s.p0 - a.window + 1 > 0 ? s.p0 - a.window + 1 : 0;
   s.lo = s.lo < s.kend ? s.lo : s.kend;
   return s;

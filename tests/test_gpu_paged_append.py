@@ -71,6 +71,11 @@ def test_rows_of_no_place(packed):
     check_append(call, "f32", 32, 2, 2, in_place=True)
 
 
+@pytest.mark.parametrize("packed", [False, True])
+def test_lengths_of_any_size(packed):
+    check_append(pr.Call([2 ** 31 - 1, -2 ** 31, 2 ** 30, 30], [8] * 4, 16, packed, width=5), "bf16", 64, 4, 2)
+
+
 def test_empty_and_many_packed_sequences():
     new = [(b * 7) % 4 for b in range(150)]              # many of them without a token
     check_append(pr.Call([20 + b % 13 for b in range(150)], new, 16, True), "bf16", 64, 2, 1)

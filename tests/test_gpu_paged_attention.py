@@ -215,6 +215,27 @@ def test_lengths_past_the_table(dtype, n):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 4, 50])
+@pytest.mark.parametrize("packed", [False, True])
+def test_lengths_of_any_size(dtype, n, packed):
+    """Past the table by far: without a window such tokens see all of it, with the weights of
+    those right behind it, and with one nothing."""
+    lengths = [2 ** 31 - 1, 2 ** 30 + 64 + n, 2 ** 25, 64 + n]
+    check_attention(pr.Call(lengths, [n] * 4, 16, packed, width=4), dtype, 64, 4, 2)
+    for width in (4, 200):                                     # (whole items, and cut ones)
+        call = pr.Call(lengths[:3], [n] * 3, 16, packed, width=width)
+        cache, q = pools(call, dtype, 2, 64), rand((*call.tokens(), 4, 64), dtype, 9).cuda()
+        (table, far), kw = call.device_args()
+        near = torch.full_like(far, call.cap + n)
+        biased = dict(slopes=slopes_of(4).cuda(), **kw)
+        want = paged_attention(q, cache, table, near, **biased)
+        assert want.any() and torch.equal(paged_attention(q, cache, table, far, **biased), want)
+        for window in (1, 16, 1000, 1 << 24):
+            out = paged_attention(q, cache, table, far, window=window, out=torch.full_like(q, 7.0), **biased)
+            assert not out.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("n", [4, 60])
 def test_inf_and_nan_reach_only_who_sees_them(dtype, n):
     """The last token's key and value are seen by its own query alone, a window's first
