@@ -111,6 +111,15 @@ const gm_paged_cache* cache_at(PyObject* address) {
   if (PyErr_Occurred()) throw Refused();
   return c;
 }
+// The pools of a cache, (k, v) or k alone: the struct holds the addresses that they had when
+// it was made, and calls are refused once they lie elsewhere (resized, or given other memory).
+const at::Tensor& pool_of(PyObject* o, const gm_paged_cache* c) {
+  const bool both = PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 2;
+  const at::Tensor& k = tensor(both ? PyTuple_GET_ITEM(o, 0) : o, "the cache");
+  if (k.data_ptr() != c->k || (both && tensor(PyTuple_GET_ITEM(o, 1), "the cache").data_ptr() != c->v))
+    refuse("the cache's k or v is not where it was when the cache was made");
+  return k;
+}
 hipStream_t stream_at(PyObject* handle) {
   void* s = PyLong_AsVoidPtr(handle);
   if (PyErr_Occurred()) throw Refused();
@@ -149,13 +158,13 @@ PyObject* guarded(F f) {
   return nullptr;
 }
 
-// (cache address, cache k, k, v, table, lengths, offsets, cos, sin, q, q_out, stream)
+// (cache address, its pools, k, v, table, lengths, offsets, cos, sin, q, q_out, stream)
 PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     if (n != 12) refuse("12 arguments are wanted");
-    const at::Tensor &pool = tensor(a[1], "the cache"), &k = tensor(a[2], "k"), &v = tensor(a[3], "v");
     gm_paged_append_args g;
     g.cache = cache_at(a[0]);
+    const at::Tensor &pool = pool_of(a[1], g.cache), &k = tensor(a[2], "k"), &v = tensor(a[3], "v");
     g.rows = places(k, "k", a[4], a[5], a[6], pool);
     const int64_t hd = g.cache->head_dim;
     g.k = rows(k, "k", k, g.cache->heads, hd, pool);
@@ -197,13 +206,13 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (cache address, cache k, q, table, lengths, offsets, window, softcap, slopes, scale, out, stream)
+// (cache address, its pools, q, table, lengths, offsets, window, softcap, slopes, scale, out, stream)
 PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     if (n != 12) refuse("12 arguments are wanted");
-    const at::Tensor &pool = tensor(a[1], "the cache"), &q = tensor(a[2], "q");
     gm_paged_attention_args g;
     g.cache = cache_at(a[0]);
+    const at::Tensor &pool = pool_of(a[1], g.cache), &q = tensor(a[2], "q");
     g.rows = places(q, "q", a[3], a[4], a[5], pool);
     const int64_t heads = q.size(q.dim() - 2);
     g.n_heads = small(heads, "the number of heads");

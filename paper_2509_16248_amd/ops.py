@@ -303,7 +303,7 @@ class PagedCache:
 
     @classmethod
     def of(cls, k: torch.Tensor, v: torch.Tensor) -> "PagedCache":
-        """The cache that lives in these two tensors."""
+        """The cache that lives in these two tensors, whose memory may not be replaced."""
         cache = cls.__new__(cls)
         cache._set(k, v)
         return cache
@@ -323,7 +323,8 @@ class PagedCache:
             raise ValueError("page_size must be 16, 32, 64, 128 or 256")
         if not 1 <= self.pages < 1 << 31 or not 1 <= self.heads <= 1 << 16:
             raise ValueError("pages and heads must be positive, pages below 2^31, heads at most 2^16")
-        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
+        # (the C struct holds their addresses, which every call compares)
+        self._pools, self.dtype, self.device = (k, v), k.dtype, k.device
         self.c = gm.gm_paged_cache(code, self.pages, self.page_size, self.heads, self.head_dim,
                                    k.data_ptr(), v.data_ptr())
         self._address = ctypes.addressof(self.c)
@@ -332,6 +333,14 @@ class PagedCache:
         self._on_gpu = k.is_cuda
         if self._on_gpu:
             self._calls = gm.torch_lib()
+
+    @property
+    def k(self) -> torch.Tensor:
+        return self._pools[0]
+
+    @property
+    def v(self) -> torch.Tensor:
+        return self._pools[1]
 
     def _away(self, stream) -> bool:
         """Whether a call has to change the device or the stream."""
@@ -354,10 +363,10 @@ class PagedCache:
         cos, sin = rotary if rotary is not None else (None, None)
         if self._away(stream):
             with _there(self.device, stream, k, v, table, lengths, offsets, cos, sin, q, q_out,
-                        self.k, self.v):
+                        *self._pools):
                 return self.append(k, v, table, lengths, offsets=offsets, rotary=rotary, q=q,
                                    q_out=q_out)
-        rc = self._calls.append(self._address, self.k, k, v, table, lengths, offsets, cos, sin, q,
+        rc = self._calls.append(self._address, self._pools, k, v, table, lengths, offsets, cos, sin, q,
                                 q_out, _raw_stream(self._index))
         if type(rc) is int:
             raise gm.GmError(rc, "gm_paged_append")
@@ -378,10 +387,10 @@ def paged_attention(q: torch.Tensor, cache: PagedCache, table: torch.Tensor,
     window, and none in holes; one that sees nothing gives zeros.  ``n_heads``
     is a multiple of the cache's heads.  Scores as in :func:`cached_attention`."""
     if cache._away(stream):
-        with _there(cache.device, stream, q, out, table, lengths, offsets, slopes, cache.k, cache.v):
+        with _there(cache.device, stream, q, out, table, lengths, offsets, slopes, *cache._pools):
             return paged_attention(q, cache, table, lengths, offsets=offsets, window=window,
                                    softcap=softcap, slopes=slopes, scale=scale, out=out)
-    rc = cache._calls.attention(cache._address, cache.k, q, table, lengths, offsets, window, softcap,
+    rc = cache._calls.attention(cache._address, cache._pools, q, table, lengths, offsets, window, softcap,
                                 slopes, cache._scale if scale is None else scale, out,
                                 _raw_stream(cache._index))
     if type(rc) is int:

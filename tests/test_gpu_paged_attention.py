@@ -414,6 +414,17 @@ def test_wrong_calls_raise():
         paged_attention(k.cpu(), cache, t, n)
 
 
+def test_a_cache_whose_memory_was_replaced():
+    t, n = torch.zeros((1, 3), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    cache = PagedCache(4, 16, 2, 64)
+    cache.append(q, q, t, n)
+    cache.v.resize_(400, 2, 16, 64)
+    for call in (lambda: cache.append(q, q, t, n), lambda: paged_attention(q, cache, t, n)):
+        with pytest.raises(ValueError, match="not where it was"):
+            call()
+
+
 def test_nothing_to_do():
     cache = PagedCache(4, 16, 2, 64)
     t = torch.zeros((0, 3), dtype=torch.int32, device="cuda")

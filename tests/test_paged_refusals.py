@@ -211,6 +211,32 @@ def test_wrappers_refuse_bad_calls():
     assert append(cos=r[:40], sin=r[:40]) == gm.GM_E_INVAL and b"every position" in gm.lib().gm_last_error()
 
 
+def test_a_cache_whose_memory_was_replaced():
+    """Calls go by the addresses that k and v had when the cache was made."""
+    M = gm.torch_lib()
+    x, t, n = torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+
+    def made():
+        k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+        return ops.PagedCache.of(k, k.clone())
+
+    c = made()
+    for name in ("k", "v"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, torch.zeros(8, 2, 16, 64, dtype=torch.bfloat16))
+    other = torch.ones(9, 2, 16, 64, dtype=torch.bfloat16)
+    for which in ("k", "v"):
+        for replace in (lambda p: p.resize_(4000, 2, 16, 64), lambda p: p.set_(other), lambda p: setattr(p, "data", other)):
+            c = made()
+            # (a window below 0 is refused by the C entry, behind the check of the memory)
+            assert M.attention(c._address, c._pools, x, t, n, None, -1, 0.0, None, 0.1, None, 0) == gm.GM_E_INVAL
+            replace(getattr(c, which))
+            with pytest.raises(ValueError, match="not where it was"):
+                M.attention(c._address, c._pools, x, t, n, None, -1, 0.0, None, 0.1, None, 0)
+            with pytest.raises(ValueError, match="not where it was"):
+                M.append(c._address, c._pools, x, x, t, n, None, None, None, None, None, 0)
+
+
 def test_rotary_tables():
     """Against the angles by Python's own arithmetic, rounded once: half a step of float32 of the
     value, and what an angle of up to 5000 loses in float64, 5000 * 2^-52."""
