@@ -179,6 +179,8 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       g.rot = small(2 * cos.size(1), "r");
       g.cos = static_cast<const float*>(array(a[7], "cos", at::kFloat, {cos.size(0), cos.size(1)}, pool));
       g.sin = static_cast<const float*>(array(a[8], "sin", at::kFloat, {cos.size(0), cos.size(1)}, pool));
+    } else if (a[8] != Py_None) {
+      refuse("sin needs cos");
     }
     g.n_q_heads = 0;
     g.q = g.q_out = gm_tensor{nullptr, 0, 0, 0};

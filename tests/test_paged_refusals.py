@@ -211,6 +211,15 @@ def test_wrappers_refuse_bad_calls():
     assert append(cos=r[:40], sin=r[:40]) == gm.GM_E_INVAL and b"every position" in gm.lib().gm_last_error()
 
 
+def test_half_a_rotary_table():
+    """cos and sin go together: neither is left out in silence."""
+    M, c, r = gm.torch_lib(), ops.PagedCache(4, 16, 2, 64, device="cpu"), torch.zeros(48, 32)
+    x, t, n = torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="sin needs cos"):
+        M.append(c._address, c._pools, x, x, t, n, None, None, r, None, None, 0)
+    assert M.append(c._address, c._pools, x, x, t, n, None, r, None, None, None, 0) == gm.GM_E_INVAL
+
+
 def test_a_cache_whose_memory_was_replaced():
     """Calls go by the addresses that k and v had when the cache was made."""
     M = gm.torch_lib()
