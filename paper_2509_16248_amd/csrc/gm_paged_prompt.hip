@@ -199,7 +199,9 @@ void k_paged_prompt(gm_paged_attention_args a, gm_paged_cache c, PromptPlan plan
   const int rw0 = w.qb * kRows + wave * 32;   // first row of this wavefront
   const bool some = rw0 < w.rows;
   const int rlast = rw0 + 31 < w.rows ? rw0 + 31 : w.rows - 1;
-  const int wmin = w.s.p0 + rw0 / plan.G, wmax = some ? w.s.p0 + rlast / plan.G : wmin - 1;
+  // positions of its first and last; a wavefront without rows copies, and skips every tile (bf16, 4
+  // sequences of 6000 keys, 32/8 heads of 128, 160 rows 46.3 -> 44.4 us, 36 rows 33.2 -> 32.7)
+  const int wmin = w.s.p0 + rw0 / plan.G, wmax = some ? w.s.p0 + rlast / plan.G : -1;
   const int r = rw0 + l32, rc = r < w.rows ? r : w.rows - 1;
   const int qi = rc / plan.G, h = kvh * plan.G + rc - qi * plan.G;
   const int qpos = w.s.p0 + qi;

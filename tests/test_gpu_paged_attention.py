@@ -138,6 +138,15 @@ def test_many_packed_sequences(dtype, B):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [9, 16, 17, 24, 25, 32, 33, 41])
+def test_blocks_with_rows_for_some_wavefronts(dtype, n):
+    """36 to 164 rows of a key head: the last block has them for one to four wavefronts of 32."""
+    check_attention(pr.Call([700, n, n + 70], [n] * 3, 16, False), dtype, 64, 8, 2)
+    check_attention(pr.Call([1500, 90], [n, n], 32, False), dtype, 128, 4, 1, window=100)
+    check_attention(pr.Call([1500, 90], [n, 8], 32, True), dtype, 32, 4, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_chunks_of_few_blocks_are_cut_up(dtype):
     check_attention(pr.Call([5000], [40], 64, False), dtype, 128, 2, 2)
     check_attention(pr.Call([5000, 1100, 300], [40, 90, 100], 64, True), dtype, 64, 2, 1)
