@@ -19,10 +19,17 @@ struct PromptPlan {
   int most;       // blocks of all sequences at the most
   int few;        // sequences of at most this many rows are another kernel's
   int split;      // keys of a block may be cut into parts
+  // Blocks of a sequence from this one on, counted from its last, come the other way round (`blocks`:
+  // none do).  Of 257 to 512 items, which run at once, the first 256 have a CU each and the others
+  // join them in order: turned round, the shortest of them joins the longest.  Us in order / turned,
+  // bf16, one prompt, 32 heads of 128: 1300 tokens 34.9 / 34.6, 1536 39.5 / 37.5, 1900 49.5 / 46.1,
+  // 2048 53.8 / 50.1; 24 heads, 2600 tokens 65.2 / 65.0, 12 heads, 4096 tokens 89.9 / 89.4.  More
+  // items run one after the other, and lose 1 to 3%.
+  int turned;
 };
 
 constexpr int kRows = 128, kKeys = 64;   // a workgroup's rows, keys of a tile
-constexpr int kSlots = 512;              // workgroups that run at a time
+constexpr int kSlots = 512;              // workgroups that run at a time, two on a CU
 // Tiles a part has at the least, and a table whose calls cut blocks at all, which takes the
 // join's launch (parts of 8 / 3 tiles: 4 packed chunks of 713 tokens of 1024, one head of 64, 24.6 /
 // 18.8 us; but 600 tokens, 12 heads of 64, whole 12.2, cut 15.5).
@@ -65,14 +72,10 @@ __device__ __forceinline__ PromptPlace prompt_place(const gm_paged_attention_arg
   w.item = static_cast<long long>(block) * c.heads + kvh;
   int qb;                                // counted from the first row
   if (p.blocks) {
-    // later tokens, which see more keys, first; sequences in turn.  Of up to 512 items, which run
-    // at once, the second 256 with their blocks the other way round, so that the two
-    // workgroups of a CU are a long and a short one (2048 tokens, 32 heads of 128: 53.6 -> 50.7
-    // us; more items run one after the other, and lose 1 to 3%).
-    const int pairs = a.rows.B * c.heads, slot = (block * c.heads) / 256;
+    // later tokens, which see more keys, first; sequences in turn (and PromptPlan::turned)
     int x = block / a.rows.B;
     w.b = block - x * a.rows.B;
-    if (256 % pairs == 0 && slot == 1 && p.most * c.heads == 512) x = 3 * (256 / pairs) - 1 - x;
+    if (x >= p.turned) x = p.turned + p.blocks - 1 - x;
     qb = p.blocks - 1 - x;
     w.s = paged_seq(a, c, w.b);
   } else {
@@ -550,6 +553,9 @@ PromptPlan prompt_plan(const gm_paged_cache& c, int B, int n, int width, int n_h
   const int64_t tiles = static_cast<int64_t>(width) * c.page_size / kKeys;
   // (of packed rows, those that must lie in blocks)
   const int64_t least = packed ? std::max<int64_t>(0, rows - static_cast<int64_t>(B) * few + kRows - 1) / kRows : p.most;
+  const int64_t pairs = static_cast<int64_t>(B) * c.heads, items = p.blocks * pairs;
+  p.turned = p.blocks;
+  if (items > kSlots / 2 && items <= kSlots) p.turned = static_cast<int>((kSlots / 2 + pairs - 1) / pairs);
   p.split = tiles >= kSplitTiles && prompt_cuts(std::max<int64_t>(least, 1) * c.heads) > 1;
   return p;
 }

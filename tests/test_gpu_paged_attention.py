@@ -106,6 +106,15 @@ def test_whole_prompts(dtype, hd, H, Hkv):
         check_attention(pr.Call([n, n], [n, n], 16, False, seed=n), dtype, hd, H, Hkv)
 
 
+@pytest.mark.parametrize("B,n,H,Hkv", [(1, 2700, 12, 12), (1, 1700, 24, 24), (3, 400, 40, 20), (1, 100, 257, 257),
+                                       (257, 70, 1, 1), (100, 200, 2, 2), (2, 1000, 32, 32), (5, 180, 68, 17),
+                                       (2, 1040, 32, 32)])
+def test_prompts_of_one_round_of_blocks(B, n, H, Hkv):
+    """More than one block of 128 rows for each of 256 workgroups, and at most two (and some more): the order
+    they come in still has every row of every sequence."""
+    check_attention(pr.Call([n + 7 * (b % 3) for b in range(B)], [n] * B, 16, False), "bf16", 32, H, Hkv)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("ps", [16, 64, 256])
 def test_chunks_behind_what_is_stored(dtype, ps):
