@@ -445,11 +445,11 @@ int gm_flush_effects(gm_model *m, gm_effect_cb cb, void *user, int32_t *n_droppe
  * tokens over it (gm_attention_cached), attention over whole prompts with
  * modified scores (gm_attention); and a cache in pages (gm_paged_append) with
  * attention over it (gm_paged_attention).  A model created with gm_model_create_ex
- * runs the same kernels.  They only enqueue on `stream`: no host
- * synchronisation, no allocation, capturable.  All pointers are device
- * pointers of the current device; a bad argument that the host can see gives
- * GM_E_INVAL and nothing is enqueued.  Calls that share no output and no
- * workspace may overlap. */
+ * runs the kernels of the first four; none runs those over pages.  They only
+ * enqueue on `stream`: no host synchronisation, no allocation, capturable.  All
+ * pointers are device pointers of the current device; a bad argument that the
+ * host can see gives GM_E_INVAL and nothing is enqueued.  Calls that share no
+ * output and no workspace may overlap. */
 
 /* A tensor [batch, tokens, heads, head_dim] whose channels are contiguous:
  * element (b, t, h, c) is at p[b * batch + t * token + h * head + c], strides
@@ -593,8 +593,8 @@ int gm_paged_append(const gm_paged_append_args* a, hipStream_t stream);
  * gives zeros, and what a hidden key or value holds, Inf and NaN among it, does not
  * reach it.  q and out: n_heads heads of cache->dtype, n_heads a multiple of
  * cache->heads, query head h reading key head h / (n_heads / cache->heads).
- * Scores, softmax statistics and sums are fp32; 16-bit probabilities are rounded
- * to the type.
+ * Scores (held times log2(e), so that they end at 2^127), softmax statistics and
+ * sums are fp32; 16-bit probabilities are rounded to the type.
  * workspace: device, 16-byte aligned, at least gm_paged_attention_workspace(...)
  * bytes (which may be 0: then NULL will do; 0 too for sizes that the call
  * refuses), used by this call alone until it has run.  `packed`: with offsets. */

@@ -279,8 +279,8 @@ constexpr int kTiles = 2048;      // key tiles a workgroup keeps marks for (1310
 // nothing.  For the others wavefront 0 fetches mask and documents with the tile.
 // SPARSE (masks or documents given) holds all of that; without it the kernel is half as
 // long, which 8192 tokens in rows of 128, causal, feel in 57.5 against 46.5 us.
-// Probabilities are rounded to T for the second product (half a step of each, 2^-9 or
-// 2^-12 of it; their sum takes them unrounded): its operands are 16-bit.
+// Probabilities are rounded to T for the second product (half a step of each, up to 2^-8
+// or 2^-11 of it; their sum takes them unrounded): its operands are 16-bit.
 // Measured, launches one after the other, 32 heads of 128, bf16, causal: 2048 tokens 56.7
 // us (606 TFLOP/s), capped 65.9, biased 60.0, both 69.6; without the causal mask 75.2 us
 // (914 TFLOP/s), capped 94.2; 8192 tokens and 8 key heads 535 us (1028 TFLOP/s), in 7 equal

@@ -281,8 +281,8 @@ constexpr int rows_waves(int hd, int nset) { return hd == 128 || nset == 2 ? 2 :
 // slots of its operand of P: P needs no exchange.  V comes in rows, HD / 16 channels of a
 // key a lane, row m of product e being channel (HD / 16) m + e; in 16 bits a byte permute per
 // word puts two keys of a channel together.
-// 16-bit weights are rounded to the type for the second product (half a step of each, 2^-9 or
-// 2^-12 of it; their sum takes them unrounded): its operands are 16-bit.
+// 16-bit weights are rounded to the type for the second product (half a step of each, up to 2^-8
+// or 2^-11 of it; their sum takes them unrounded): its operands are 16-bit.
 // The two tiles of NSET = 1 take 64 registers each at 128 channels; with 32 rows there is one,
 // whose K and V are fetched again as soon as each has been used.
 // The maximum m moves lazily (by more than 2^8).  Hidden keys have weight 0, and values that
@@ -744,9 +744,14 @@ constexpr int kFewRows = 32;
 // 128, five tokens, 24.3 / 39.6 / 43.3; 32 of 1000 25.1 / 32.0 / 33.1, of 8190 159 / 162 / 164;
 // one of 1000 15.4 / 13.6 / 12.4, of 32000 with 32 key heads 350 / 98.5 / 100; four of 1500 20.6
 // / 14.8 / 15.7; one of 8190 among 31 of 300 102 / 27.8 / 29.5).  Only the table's capacity is
-// known on the host, so an item that could take 25 us is never whole: the lengths may be
-// anything.  8 wavefronts a whole item: 16 sequences of 1000 keys, 8 heads of 32, 8.4 us, with 4
-// 9.7; 2048 items of 700 keys 103.8 and 102.6.
+// known on the host, so of fewer than 1024 items one that could take 25 us is never whole: the
+// lengths may be anything.  More items are whole whatever they could take: they fill the chip four
+// times, so that equal lengths lose by sharing, though uneven ones would gain (us whole / shared;
+// 32 sequences, 32 heads of 128, of 300 keys in a table of 8192 positions 32.5 / 43.3, of 1000 92.5 /
+// 100.5, of 8000 700 / 705, one of 32000 among 31 of 300 383 / 127; 32/8 heads, 128 sequences of
+// 4000 to 8000 524 / 542, of 100 to 8000 220 / 186, 512 of 500 186 / 209).  8 wavefronts a whole
+// item: 16 sequences of 1000 keys, 8 heads of 32, 8.4 us, with 4 9.7; 2048 items of 700 keys 103.8
+// and 102.6.
 
 PagedWay paged_way(const gm_paged_cache& c, int B, int n, int width, int n_heads, int window, bool packed) {
   PagedWay w;

@@ -161,8 +161,8 @@ constexpr int paged_prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 :
 // 2048 tokens below; so 52.9.)
 // LDS is read ahead of the products by hand: K two k steps, V one of 16 keys (left to the
 // compiler each K operand's read waits for the one before: 2 us more).
-// Probabilities are rounded to T for the second product (half a step of each, 2^-9 or 2^-12
-// of it; their sum takes them unrounded): its operands are 16-bit.
+// Probabilities are rounded to T for the second product (half a step of each, up to 2^-8 or
+// 2^-11 of it; their sum takes them unrounded): its operands are 16-bit.
 // A hidden key has probability 0, but 0 times an Inf or NaN value is NaN in the matrix
 // product: rows whose sums came out not finite are computed again by paged_row, which skips
 // hidden keys.
