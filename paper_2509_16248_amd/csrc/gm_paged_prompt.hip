@@ -169,7 +169,7 @@ constexpr int paged_prompt_waves(int hd) { return hd == 128 ? 2 : hd == 64 ? 3 :
 // Measured, bf16, 32 heads of 128, launches one after the other: 2048 tokens 48 to 51 us (700
 // TFLOP/s; capped 57, biased 56), 4 x 2048 with 8 key heads 154 (890), 8192 tokens 530 (1040; a
 // large matrix product reaches 1197), 512 tokens behind 7680 85 (770).  What bounds it: a SIMD's
-// two wavefronts keep the matrix cores busy 50% and the vector units 43% of the time that CUs
+// two wavefronts keep the matrix cores busy 49% and the vector units 42% of the time that CUs
 // hold work, each wavefront's own chain of instructions taking the rest.  Not faster: the next
 // tile's scores beside this one's probabilities in one wavefront (the registers of two score
 // tiles spill, 2 x slower; at one wavefront per SIMD without spilling 1.6 x), halves of a tile
